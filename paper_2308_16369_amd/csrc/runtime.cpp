@@ -61,7 +61,9 @@ size_t esize(const sarathi_model_cfg* c) { return c->dtype == SARATHI_BF16 ? 2 :
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-int check_cfg(const sarathi_model_cfg* c) {
+}  // namespace
+
+int sarathi::check_cfg(const sarathi_model_cfg* c) {
   if (!c) return fail(SARATHI_EINVAL, "cfg is NULL");
   if (c->dtype != SARATHI_F32 && c->dtype != SARATHI_BF16)
     return fail(SARATHI_EUNSUPPORTED, "dtype %d not supported (F32 or BF16)", c->dtype);
@@ -81,6 +83,8 @@ int check_cfg(const sarathi_model_cfg* c) {
   if (!(c->eps > 0.0f)) return fail(SARATHI_EINVAL, "eps must be > 0");
   return SARATHI_OK;
 }
+
+namespace {
 
 bool same_cfg(const sarathi_model_cfg* a, const sarathi_model_cfg* b) {
   return a->hidden == b->hidden && a->n_heads == b->n_heads && a->head_dim == b->head_dim && a->ffn == b->ffn &&
@@ -121,23 +125,6 @@ Layout make_layout(const sarathi_model_cfg* c, int T, int n_chunks, int S) {
   return L;
 }
 
-// A batch of any number of prompt chunks plus decodes (the hybrid batch of
-// the paper has at most one chunk).
-struct ChunkDesc {
-  int slot, offset, len;
-};
-struct BatchDesc {
-  std::vector<ChunkDesc> chunks;
-  int B = 0;
-  const int* dslots = nullptr;
-  const int* dctx = nullptr;
-  int rows() const {
-    int r = B;
-    for (const ChunkDesc& c : chunks) r += c.len;
-    return r;
-  }
-};
-
 int from_hybrid(const sarathi_hybrid_batch* b, BatchDesc* out) {
   if (!b) return fail(SARATHI_EINVAL, "batch is NULL");
   if (b->chunk_len < 0) return fail(SARATHI_ERANGE, "chunk_len %d < 0", b->chunk_len);
@@ -150,7 +137,9 @@ int from_hybrid(const sarathi_hybrid_batch* b, BatchDesc* out) {
   return SARATHI_OK;
 }
 
-int from_mixed(const sarathi_mixed_batch* b, BatchDesc* out) {
+}  // namespace
+
+int sarathi::from_mixed(const sarathi_mixed_batch* b, BatchDesc* out) {
   if (!b) return fail(SARATHI_EINVAL, "batch is NULL");
   if (b->n_chunks < 0 || b->n_chunks > (1 << 16)) return fail(SARATHI_EINVAL, "n_chunks %d out of range", b->n_chunks);
   if (b->n_decodes < 0) return fail(SARATHI_EINVAL, "n_decodes %d < 0", b->n_decodes);
@@ -167,6 +156,8 @@ int from_mixed(const sarathi_mixed_batch* b, BatchDesc* out) {
   return SARATHI_OK;
 }
 
+namespace {
+
 // Host-side description of the batch and its device metadata.
 struct Plan {
   int C, B, T, row_base, n_pre, n_dec, n_chunks, pre_tiles;
@@ -180,17 +171,19 @@ struct Plan {
   size_t o_slot, o_pos, o_comb, o_chunks, o_pre, o_dec;   // int offsets into meta
 };
 
-int check_batch(const sarathi_model_cfg* cfg, const sarathi_kv* kv, const BatchDesc& b) {
-  const int B = b.B, S = kv->max_seq_len;
+}  // namespace
+
+int sarathi::check_batch(const BatchDesc& b, int n_slots, int S) {
+  const int B = b.B;
   long rows = B;
   for (const ChunkDesc& c : b.chunks) rows += c.len;
   if (rows == 0) return fail(SARATHI_EINVAL, "empty batch (no chunk rows and no decodes)");
   if (rows > (1 << 19)) return fail(SARATHI_EINVAL, "batch of %ld rows too large", rows);
-  std::vector<char> used(kv->n_slots, 0);
+  std::vector<char> used(n_slots, 0);
   for (size_t i = 0; i < b.chunks.size(); ++i) {
     const ChunkDesc& c = b.chunks[i];
-    if (c.slot < 0 || c.slot >= kv->n_slots)
-      return fail(SARATHI_EINVAL, "chunk %zu: slot %d outside [0, %d)", i, c.slot, kv->n_slots);
+    if (c.slot < 0 || c.slot >= n_slots)
+      return fail(SARATHI_EINVAL, "chunk %zu: slot %d outside [0, %d)", i, c.slot, n_slots);
     if (used[c.slot]) return fail(SARATHI_EINVAL, "slot %d appears twice in the batch", c.slot);
     used[c.slot] = 1;
     if (c.offset < 0) return fail(SARATHI_ERANGE, "chunk %zu: offset %d < 0", i, c.offset);
@@ -201,16 +194,17 @@ int check_batch(const sarathi_model_cfg* cfg, const sarathi_kv* kv, const BatchD
     if (!b.dslots || !b.dctx) return fail(SARATHI_EINVAL, "decode arrays are NULL");
     for (int i = 0; i < B; ++i) {
       const int s = b.dslots[i], ctx = b.dctx[i];
-      if (s < 0 || s >= kv->n_slots) return fail(SARATHI_EINVAL, "decode_slots[%d] = %d outside [0, %d)", i, s, kv->n_slots);
+      if (s < 0 || s >= n_slots) return fail(SARATHI_EINVAL, "decode_slots[%d] = %d outside [0, %d)", i, s, n_slots);
       if (used[s]) return fail(SARATHI_EINVAL, "slot %d appears twice in the batch", s);
       used[s] = 1;
       if (ctx < 0) return fail(SARATHI_ERANGE, "decode_ctx_lens[%d] = %d < 0", i, ctx);
       if ((long)ctx + 1 > S) return fail(SARATHI_ERANGE, "decode_ctx_lens[%d] + 1 = %d > max_seq_len %d", i, ctx + 1, S);
     }
   }
-  (void)cfg;
   return SARATHI_OK;
 }
+
+namespace {
 
 Plan make_plan(const sarathi_model_cfg* cfg, const BatchDesc& b) {
   Plan p;
@@ -372,7 +366,9 @@ Plan make_plan(const sarathi_model_cfg* cfg, const BatchDesc& b) {
   return p;
 }
 
-int check_weights(const sarathi_model_cfg* cfg, const sarathi_layer_weights* w, int layer) {
+}  // namespace
+
+int sarathi::check_weights(const sarathi_model_cfg* cfg, const sarathi_layer_weights* w, int layer) {
   if (!w) return fail(SARATHI_EINVAL, "weights are NULL");
   const void* need[] = {w->norm1_g, w->w_qkv, w->w_o, w->norm2_g, w->w_up, w->w_down};
   for (const void* p : need)
@@ -386,6 +382,8 @@ int check_weights(const sarathi_model_cfg* cfg, const sarathi_layer_weights* w, 
   }
   return SARATHI_OK;
 }
+
+namespace {
 
 // ---- stage timing: a pool of HIP events recorded at stage boundaries.
 constexpr int EV_PER_CALL = SARATHI_N_STAGES + 1;
@@ -590,7 +588,7 @@ int check_call(const sarathi_model_cfg* cfg, const sarathi_layer_weights* w, int
   if (rc) return rc;
   if (!kv) return fail(SARATHI_EINVAL, "kv is NULL");
   if (!same_cfg(cfg, &kv->cfg)) return fail(SARATHI_EINVAL, "cfg differs from the cfg the KV cache was bound with");
-  rc = check_batch(cfg, kv, batch);
+  rc = check_batch(batch, kv->n_slots, kv->max_seq_len);
   if (rc) return rc;
   for (int i = 0; i < n_w; ++i) {
     rc = check_weights(cfg, w + i, i);

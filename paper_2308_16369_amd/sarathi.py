@@ -1,4 +1,5 @@
-"""ctypes binding of libsarathi.so (see include/sarathi.h for the contract).
+"""ctypes binding of libsarathi.so (see include/sarathi.h, sarathi_sched.h and
+sarathi_kv8.h for the contract).
 
 Argument marshalling only: every step of the layer runs in the library's HIP
 kernels.  The names mirror the C entry points.  Device memory is passed as
@@ -24,6 +25,9 @@ F32, BF16 = 0, 1
 NORM_RMS, NORM_LAYER = 0, 1
 ACT_SWIGLU, ACT_GELU = 0, 1
 LINEAR_PLAIN, LINEAR_RESID, LINEAR_RESID_F32IN, LINEAR_SWIGLU, LINEAR_GELU = 0, 1, 2, 3, 4
+KV8_INT8, KV8_E4M3 = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS = 0, 1, 2, 3
 POLICY_DECODE_MAXIMAL, POLICY_PREFILL_DECODE, POLICY_MIXED = 0, 1, 2
 
 _ERRNAMES = {EINVAL: "EINVAL", ERANGE: "ERANGE", ENOSPC: "ENOSPC", EUNSUPPORTED: "EUNSUPPORTED", EHIP: "EHIP"}
@@ -74,6 +78,18 @@ class sarathi_ws_layout(ct.Structure):
 class sarathi_attn_plan(ct.Structure):
     _fields_ = [("chunk_items", ct.c_int), ("decode_items", ct.c_int), ("partial_rows_written", ct.c_long),
                 ("partial_rows_read", ct.c_long), ("combine_rows", ct.c_int)]
+
+
+class sarathi_kv8_cfg(ct.Structure):
+    _fields_ = [(n, ct.c_int) for n in ("n_heads", "n_kv_heads", "head_dim", "n_layers", "dtype", "format", "block")] + \
+        [("softmax_scale", ct.c_float), ("qk_norm", ct.c_int), ("qk_eps", ct.c_float), ("rope_dim", ct.c_int),
+         ("rope_layout", ct.c_int), ("rope_scaling", ct.c_int), ("rope_base", ct.c_float), ("rope_factor", ct.c_float),
+         ("rope_low", ct.c_float), ("rope_high", ct.c_float), ("rope_orig_len", ct.c_int), ("rope_mscale", ct.c_float)]
+
+
+class sarathi_kv8_layout(ct.Structure):
+    _fields_ = [(n, ct.c_size_t) for n in ("layer", "slot", "kv", "head", "pos", "scale_layer", "scale_slot", "scale_kv",
+                                           "scale_head", "scale_offset")]
 
 
 class sarathi_sched_cfg(ct.Structure):
@@ -141,6 +157,21 @@ EXPORTS = {
     "sarathi_linear_tiled": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_void_p, ct.c_void_p,
                                         ct.c_void_p, ct.c_void_p, ct.c_void_p, ct.c_size_t, ct.c_int, ct.c_int,
                                         ct.c_void_p]),
+    "sarathi_kv8_bytes": (ct.c_size_t, [ct.POINTER(sarathi_kv8_cfg), ct.c_int, ct.c_int]),
+    "sarathi_kv8_alloc": (ct.c_int, [ct.POINTER(sarathi_kv8_cfg), ct.c_int, ct.c_int, ct.c_void_p, ct.c_size_t,
+                                     ct.POINTER(ct.c_void_p)]),
+    "sarathi_kv8_free": (None, [ct.c_void_p]),
+    "sarathi_kv8_get_layout": (ct.c_int, [ct.c_void_p, ct.POINTER(sarathi_kv8_layout)]),
+    "sarathi_kv8_plan_bytes": (ct.c_size_t, [ct.POINTER(sarathi_kv8_cfg), ct.c_int, ct.c_int, ct.c_int]),
+    "sarathi_kv8_plan_create": (ct.c_int, [ct.c_void_p, ct.POINTER(sarathi_mixed_batch), ct.c_void_p, ct.c_size_t,
+                                           ct.c_void_p, ct.POINTER(ct.c_void_p)]),
+    "sarathi_kv8_plan_free": (None, [ct.c_void_p]),
+    "sarathi_kv8_append": (ct.c_int, [ct.c_void_p, ct.c_int, ct.c_void_p, ct.c_size_t, ct.c_void_p, ct.c_void_p,
+                                      ct.c_void_p, ct.c_size_t, ct.c_void_p]),
+    "sarathi_kv8_attention": (ct.c_int, [ct.c_void_p, ct.c_int, ct.c_void_p, ct.c_size_t, ct.c_void_p, ct.c_size_t,
+                                         ct.c_void_p]),
+    "sarathi_kv8_read": (ct.c_int, [ct.c_void_p, ct.c_int, ct.c_int, ct.c_void_p, ct.c_size_t, ct.c_void_p,
+                                    ct.c_size_t, ct.c_void_p]),
     "sarathi_sched_create": (ct.c_int, [ct.POINTER(sarathi_sched_cfg), ct.POINTER(ct.c_void_p)]),
     "sarathi_sched_destroy": (None, [ct.c_void_p]),
     "sarathi_sched_submit": (ct.c_int, [ct.c_void_p, ct.c_int, ct.c_int, ct.POINTER(ct.c_int)]),
@@ -382,6 +413,95 @@ def sarathi_linear_tiled(kind, M, N, K, x: int, w: int, resid: int, out: int, sc
     rc = lib().sarathi_linear_tiled(kind, M, N, K, ct.c_void_p(x), ct.c_void_p(w), ct.c_void_p(resid or None),
                                     ct.c_void_p(out), ct.c_void_p(scratch or None), scratch_bytes, tile, n_split,
                                     ct.c_void_p(stream))
+    return _check(rc) if check else rc
+
+
+# ---------------------------------------------------------------------------- 8-bit KV cache
+
+def make_kv8_cfg(n_heads, n_kv_heads, head_dim, n_layers=1, dtype=BF16, format=KV8_INT8, block=32, softmax_scale=0.0,
+                 qk_norm=0, qk_eps=1e-6, rope_dim=0, rope_layout=ROPE_HALF, rope_scaling=ROPE_PLAIN, rope_base=10000.0,
+                 rope_factor=1.0, rope_low=1.0, rope_high=32.0, rope_orig_len=0, rope_mscale=0.0) -> sarathi_kv8_cfg:
+    return sarathi_kv8_cfg(n_heads, n_kv_heads, head_dim, n_layers, dtype, format, block, softmax_scale, qk_norm, qk_eps,
+                           rope_dim, rope_layout, rope_scaling, rope_base, rope_factor, rope_low, rope_high,
+                           rope_orig_len, rope_mscale)
+
+
+def sarathi_kv8_bytes(cfg: sarathi_kv8_cfg, n_slots: int, max_seq_len: int) -> int:
+    return lib().sarathi_kv8_bytes(ct.byref(cfg), n_slots, max_seq_len)
+
+
+class _Handle:
+    """Owner of one host object of the library."""
+
+    _free = ""
+
+    def free(self):
+        if self.handle:
+            getattr(lib(), self._free)(self.handle)
+            self.handle = ct.c_void_p()
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+class KV8(_Handle):
+    """Host handle of an 8-bit KV cache bound to caller-owned device memory."""
+
+    _free = "sarathi_kv8_free"
+
+    def __init__(self, cfg: sarathi_kv8_cfg, n_slots: int, max_seq_len: int, dev_ptr: int, dev_bytes: int):
+        self.handle = ct.c_void_p()
+        _check(lib().sarathi_kv8_alloc(ct.byref(cfg), n_slots, max_seq_len, ct.c_void_p(dev_ptr), dev_bytes,
+                                       ct.byref(self.handle)))
+        self.cfg, self.n_slots, self.max_seq_len = cfg, n_slots, max_seq_len
+
+    def layout(self) -> sarathi_kv8_layout:
+        out = sarathi_kv8_layout()
+        _check(lib().sarathi_kv8_get_layout(self.handle, ct.byref(out)))
+        return out
+
+
+def sarathi_kv8_alloc(cfg, n_slots, max_seq_len, dev_ptr, dev_bytes) -> KV8:
+    return KV8(cfg, n_slots, max_seq_len, dev_ptr, dev_bytes)
+
+
+def sarathi_kv8_plan_bytes(cfg: sarathi_kv8_cfg, max_tokens: int, max_chunks: int, max_seq_len: int) -> int:
+    return lib().sarathi_kv8_plan_bytes(ct.byref(cfg), max_tokens, max_chunks, max_seq_len)
+
+
+class KV8Plan(_Handle):
+    """The plan of one mixed batch (make_mixed_batch) over a KV8, in device memory at ws."""
+
+    _free = "sarathi_kv8_plan_free"
+
+    def __init__(self, kv: KV8, batch, ws: int, ws_bytes: int, stream: int = 0):
+        self.handle = ct.c_void_p()
+        _check(lib().sarathi_kv8_plan_create(kv.handle, ct.byref(batch), ct.c_void_p(ws), ws_bytes, ct.c_void_p(stream),
+                                             ct.byref(self.handle)))
+
+
+def sarathi_kv8_plan_create(kv: KV8, batch, ws: int, ws_bytes: int, stream: int = 0) -> KV8Plan:
+    return KV8Plan(kv, batch, ws, ws_bytes, stream)
+
+
+def sarathi_kv8_append(plan: KV8Plan, layer: int, qkv: int, ld_qkv: int, q_gain: int, k_gain: int, q_out: int, ld_q: int,
+                       stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_kv8_append(plan.handle, layer, qkv, ld_qkv, q_gain or None, k_gain or None, q_out, ld_q, stream)
+    return _check(rc) if check else rc
+
+
+def sarathi_kv8_attention(plan: KV8Plan, layer: int, q: int, ld_q: int, out: int, ld_out: int, stream: int = 0,
+                          check: bool = True) -> int:
+    rc = lib().sarathi_kv8_attention(plan.handle, layer, q, ld_q, out, ld_out, stream)
+    return _check(rc) if check else rc
+
+
+def sarathi_kv8_read(plan: KV8Plan, layer: int, out_dtype: int, k_out: int, ld_k: int, v_out: int, ld_v: int,
+                     stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_kv8_read(plan.handle, layer, out_dtype, k_out or None, ld_k, v_out or None, ld_v, stream)
     return _check(rc) if check else rc
 
 
