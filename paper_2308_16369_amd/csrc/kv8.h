@@ -69,15 +69,19 @@ struct Kv8ReadArgs {
 };
 hipError_t launch_kv8_read(int out_dtype, int format, const Kv8ReadArgs& a, hipStream_t s);
 
-// ---- attention of decodes: one item is a range of one decode's keys.
+// ---- attention of decodes.  Item: a range of one decode's keys, [row, slot, first key, end key, partial row (-1: the
+// row's only item)].  Rows of several items are joined: [row, items, first partial row].
+constexpr int KV8_DEC_INTS = 5, KV8_JOIN_INTS = 3;
 struct Kv8DecodeArgs {
   const void* q;
   size_t ld_q;
   void* out;
   size_t ld_out;
-  const int* work;              // [n_work][5]: row, slot, key begin, key end, partial (-1: the row's only item)
+  const int* work;              // [n_work][KV8_DEC_INTS]
+  const int* joins;             // [n_joins][KV8_JOIN_INTS]
+  int n_joins;
   int n_work, nh, nkv;
-  float* part;
+  float* part;                  // partial rows (kernels.h)
   float scale_log2;             // softmax scale * log2 e
   Kv8Layer kv;
 };

@@ -17,6 +17,16 @@
 // by reading the cache).  A scale is constant over 16 keys: the key scale
 // multiplies the scores with the softmax scale, the value scale the
 // probabilities.
+//
+// bf16 rows over int8 codes multiply in f16 instead, whose subnormals make the
+// conversion of a code a byte move: u = code + 128 (one xor per four codes) put
+// into the low byte of a half is u 2^-24.  The offset goes out at the end,
+//   q . code = 2^24 q . (u 2^-24) - 128 sum(q),
+// and alike for V with the sum of the probabilities.  q is scaled by a power of
+// two into f16's range (its 8 bits fit; elements below 2^-28 of the row's
+// largest lose bits), and the probabilities times their value scale are kept
+// near one by a running maximum of their own (the scales may differ by any
+// factor), so they keep 11 bits.
 #include "kv8.h"
 
 namespace sarathi {
@@ -87,9 +97,24 @@ __device__ __forceinline__ void split8(const float* x, bf16x8_t* t) {
   }
 }
 
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pk_f16(float a, float b) {   // nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
+}
+
+template <typename T>
+__device__ __forceinline__ void store_out4(const Kv8DecodeArgs& a, int row, int head, int D, int d, floatx4 x) {
+  T* out = reinterpret_cast<T*>(a.out) + (size_t)row * a.ld_out + (size_t)head * D + d;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]));
+  else *reinterpret_cast<floatx4*>(out) = x;
+}
+
+// F16 (bf16 rows over int8 codes): see the file comment.
 template <typename T, int D, bool INT8>
-__global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
   constexpr int NT = sizeof(T) == 2 ? 1 : 3;
+  constexpr bool F16 = INT8 && NT == 1;
   constexpr int KI = D / 64;             // 16-byte K loads per key row and lane
   constexpr int DB = D / 16;             // V bytes per key row and lane; tiles of O
   constexpr int VW = DB / 4;             // dwords of them
@@ -104,7 +129,7 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, gq = lane >> 4;
-  const int* wk = a.work + 5 * item;
+  const int* wk = a.work + KV8_DEC_INTS * item;
   const int row = wk[0], slot = wk[1], kb = wk[2], ke = wk[3], part = wk[4];
 
   const uint8_t* kbase = a.kv.codes + slot * a.kv.slot + kvh * a.kv.head;
@@ -112,24 +137,57 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
   const float* ksc = a.kv.scales + slot * a.kv.s_slot + kvh * a.kv.s_head;
   const float* vsc = ksc + a.kv.s_kv;
 
-  bf16x8_t qf[2 * KI][NT];
+  // scores: s = raw * (key scale * c_mul) + key scale * c_add
+  float c_mul = a.scale_log2, c_add = 0.f;
+  u32x4 qf[2 * KI][NT];
   {
-    const T* q = reinterpret_cast<const T*>(a.q) + (size_t)row * a.ld_q + (size_t)(head0 + min(c, nheads - 1)) * D;
+    const T* q = reinterpret_cast<const T*>(a.q) + (size_t)row * a.ld_q + (size_t)(head0 + min(c, nheads - 1)) * D + 16 * gq;
+    if constexpr (F16) {
+      float x[2 * KI][8], top = 0.f, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2 * KI; ++i) {
-      const T* p = q + 64 * (i / 2) + 16 * gq + 8 * (i & 1);
-      if constexpr (NT == 1) {
-        qf[i][0] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(p));
-      } else {
-        float x[8];
-        Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
-        Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
-        split8<NT>(x, qf[i]);
+      for (int i = 0; i < 2 * KI; ++i) {
+        Vec16<bf16>::unpack(*reinterpret_cast<const uint4*>(q + 64 * (i / 2) + 8 * (i & 1)), x[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+      }
+      // a power of two that brings the row's largest magnitude to 2^14 .. 2^15
+      const int ex = min(max((int)(__float_as_uint(groups_max(top)) >> 23) - 127, -100), 110) - 14;
+      const float f = __builtin_ldexpf(1.f, -ex);
+#pragma unroll
+      for (int i = 0; i < 2 * KI; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = pk_f16(x[i][2 * e] * f, x[i][2 * e + 1] * f);
+          qf[i][0][e] = w;
+          sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, w), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, sum, false);
+        }
+      c_mul = __builtin_ldexpf(a.scale_log2, ex);
+      c_add = -128.f * groups_sum(sum) * c_mul;
+      c_mul *= 16777216.f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * KI; ++i) {
+        const T* p = q + 64 * (i / 2) + 8 * (i & 1);
+        if constexpr (NT == 1) {
+          qf[i][0] = *reinterpret_cast<const u32x4*>(p);
+        } else {
+          float x[8];
+          Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
+          Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
+          bf16x8_t t[NT];
+          split8<NT>(x, t);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) qf[i][n] = __builtin_bit_cast(u32x4, t[n]);
+        }
       }
     }
   }
 
-  float m_run = -INFINITY, l_run = 0.f;   // m: of head c, the same in its four lanes; l: this lane's keys
+  // m_run: the running maximum of head c's scores (the same in its four lanes),
+  // l_run: this lane's share of the row sum, in units of 2^m_run.  F16: M_run,
+  // the running maximum of score + log2(value scale); o and lp (the sum of the
+  // rounded probabilities) are in units of 2^M_run.
+  float m_run = -INFINITY, M_run = -INFINITY, l_run = 0.f, lp = 0.f;
   floatx4 o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -137,33 +195,44 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
   struct Tile {
     u32x4_nt k[2][KI];
     uint32_t v[8][VW];
-    float ks[2], vs[2], vi[2];   // the two 16-key tiles' scales of K and V, and 1 / V's
+    float ks[2], vs[2];
+  };
+  auto load_v = [&](uint32_t* v, const uint8_t* p) {
+    if constexpr (VW == 2) {
+      const u32x2_nt w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_nt*>(p));
+      v[0] = w[0]; v[1] = w[1];
+    } else {
+      v[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+    }
   };
   // 32 keys from k0; positions past the item's end re-read its last key (masked below)
   auto load = [&](Tile& t, int k0) {
+    if (k0 + 32 <= ke) {
+      const uint8_t* kp = kbase + (size_t)(k0 + c) * D + 16 * gq;
+      const uint8_t* vp = vbase + (size_t)(k0 + 4 * gq) * D + DB * c;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < KI; ++i)
-        t.k[h][i] = __builtin_nontemporal_load(
-            reinterpret_cast<const u32x4_nt*>(kbase + (size_t)min(k0 + 16 * h + c, ke - 1) * D + 64 * i + 16 * gq));
+        for (int i = 0; i < KI; ++i)
+          t.k[h][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_nt*>(kp + 16 * h * D + 64 * i));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint8_t* p = vbase + (size_t)min(k0 + 16 * (e >> 2) + 4 * gq + (e & 3), ke - 1) * D + DB * c;
-      if constexpr (VW == 2) {
-        const u32x2_nt w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_nt*>(p));
-        t.v[e][0] = w[0]; t.v[e][1] = w[1];
-      } else {
-        t.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
-      }
+      for (int e = 0; e < 8; ++e) load_v(t.v[e], vp + (16 * (e >> 2) + (e & 3)) * D);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < KI; ++i)
+          t.k[h][i] = __builtin_nontemporal_load(
+              reinterpret_cast<const u32x4_nt*>(kbase + (size_t)min(k0 + 16 * h + c, ke - 1) * D + 64 * i + 16 * gq));
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        load_v(t.v[e], vbase + (size_t)min(k0 + 16 * (e >> 2) + 4 * gq + (e & 3), ke - 1) * D + DB * c);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int b = min(k0 + 16 * h, ke - 1) >> a.kv.log2_block;
       t.ks[h] = ksc[b];
-      const float y = vsc[b];
-      t.vs[h] = y > 0.f ? y : 1.f;      // a zero scale belongs to zero codes
-      t.vi[h] = 1.0f / t.vs[h];
+      t.vs[h] = vsc[b];
     }
   };
   auto step = [&](const Tile& t, int k0) {
@@ -175,12 +244,22 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
       for (int i = 0; i < KI; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const bf16x8_t kf = codes8_bf16<INT8>(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]);
+          if constexpr (F16) {
+            const uint32_t x = t.k[h][i][2 * u] ^ 0x80808080u, y = t.k[h][i][2 * u + 1] ^ 0x80808080u;
+            const u32x4 w{__builtin_amdgcn_perm(x, x, 0x0c010c00), __builtin_amdgcn_perm(x, x, 0x0c030c02),
+                          __builtin_amdgcn_perm(y, y, 0x0c010c00), __builtin_amdgcn_perm(y, y, 0x0c030c02)};
+            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, w),
+                                                          __builtin_bit_cast(f16x8_t, qf[2 * i + u][0]), s[h], 0, 0, 0);
+          } else {
+            const bf16x8_t kf = codes8_bf16<INT8>(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]);
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * i + u][n], s[h], 0, 0, 0);
+            for (int n = 0; n < NT; ++n)
+              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8_t, qf[2 * i + u][n]), s[h], 0, 0, 0);
+          }
         }
-      s[h] *= t.ks[h] * a.scale_log2;
+      const float mul = t.ks[h] * c_mul, add = t.ks[h] * c_add;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) s[h][v] = F16 ? fmaf(s[h][v], mul, add) : s[h][v] * mul;
     }
     if (k0 + 32 > ke) {
 #pragma unroll
@@ -189,70 +268,115 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
         for (int v = 0; v < 4; ++v)
           if (k0 + 16 * h + 4 * gq + v >= ke) s[h][v] = -INFINITY;
     }
-    // the running maximum moves only when a score exceeds it by more than 2^8
+    // the running maxima move only when exceeded by more than 2^8
     // (probabilities stay below 256; sums and products keep their precision)
-    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    mx = groups_max(mx);
-    if (__ballot(mx > m_run + 8.0f)) {
-      const float m_new = fmaxf(m_run, mx);
-      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[db] *= corr;
-      l_run *= corr;
-      m_run = m_new;
-    }
-    float p[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_run);
+    const float mx0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+    const float mx1 = fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
+    const float mx = groups_max(fmaxf(mx0, mx1));
+    uint32_t w[4];
     bf16x8_t pf[NT];
-    if constexpr (NT == 1) {
-      // the row sum takes the rounded probabilities that multiply V: the
-      // weights add up to one, whatever their rounding
-      const bf16x2_t ones = __builtin_convertvector((f32x2_t){1.f, 1.f}, bf16x2_t);
-      u32x4 w;
+    if constexpr (F16) {
+      // value scales as logarithms; a zero scale belongs to zero codes: any small one does
+      const float lv0 = __builtin_amdgcn_logf(fmaxf(t.vs[0], KV8_TINY)), lv1 = __builtin_amdgcn_logf(fmaxf(t.vs[1], KV8_TINY));
+      const float Mx = groups_max(fmaxf(mx0 + lv0, mx1 + lv1));
+      if (__ballot(mx > m_run + 8.0f || Mx > M_run + 8.0f)) {
+        const float m_new = fmaxf(m_run, mx), M_new = fmaxf(M_run, Mx);
+        l_run *= m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        const float corr = M_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M_run - M_new);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= corr;
+        lp *= corr;
+        m_run = m_new;
+        M_run = M_new;
+      }
+      const float d = M_run - m_run;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float sum = 0.f;
+        const float lv = h ? lv1 : lv0, add = lv - M_run;
+        float p[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) p[v] = __builtin_amdgcn_exp2f(s[h][v] + add);
+        // back to units of 2^m_run and no value scale
+        l_run = fmaf((p[0] + p[1]) + (p[2] + p[3]), __builtin_amdgcn_exp2f(fminf(d - lv, 126.f)), l_run);
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          const uint32_t pair = pk_bf16(p[4 * h + 2 * v] * t.vs[h], p[4 * h + 2 * v + 1] * t.vs[h]);
+          const uint32_t pair = pk_f16(p[2 * v], p[2 * v + 1]);
           w[2 * h + v] = pair;
-          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), ones, sum, false);
+          lp = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pair), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, lp, false);
         }
-        l_run = fmaf(sum, t.vi[h], l_run);
       }
-      pf[0] = __builtin_bit_cast(bf16x8_t, w);
     } else {
+      if (__ballot(mx > m_run + 8.0f)) {
+        const float m_new = fmaxf(m_run, mx);
+        const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        l_run += p[i];
-        p[i] *= t.vs[i >> 2];
+        for (int db = 0; db < DB; ++db) o[db] *= corr;
+        l_run *= corr;
+        m_run = m_new;
       }
-      split8<NT>(p, pf);
+      float p[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_run);
+      if constexpr (NT == 1) {
+        // the row sum takes the rounded probabilities that multiply V: the
+        // weights add up to one, whatever their rounding
+        const bf16x2_t ones = __builtin_convertvector((f32x2_t){1.f, 1.f}, bf16x2_t);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float vs = t.vs[h] > 0.f ? t.vs[h] : 1.f;      // a zero scale belongs to zero codes
+          float sum = 0.f;
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t pair = pk_bf16(p[4 * h + 2 * v] * vs, p[4 * h + 2 * v + 1] * vs);
+            w[2 * h + v] = pair;
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), ones, sum, false);
+          }
+          l_run = fmaf(sum, 1.0f / vs, l_run);
+        }
+        pf[0] = __builtin_bit_cast(bf16x8_t, u32x4{w[0], w[1], w[2], w[3]});
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          l_run += p[i];
+          p[i] *= t.vs[i >> 2];
+        }
+        split8<NT>(p, pf);
+      }
     }
 #pragma unroll
-    for (int w = 0; w < VW; ++w) {
-      // bytes 4 w .. + 3 of the eight keys' rows, as four vectors over the keys
-      uint32_t x[4][4];
+    for (int x = 0; x < VW; ++x) {
+      // bytes 4 x .. + 3 of the eight keys' rows, as four vectors over the keys
+      uint32_t y[4][4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        uint32_t lo0, hi0, lo1, hi1;
-        codes_bf16<INT8>(t.v[2 * e][w], lo0, hi0);
-        codes_bf16<INT8>(t.v[2 * e + 1][w], lo1, hi1);
-        x[0][e] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100);
-        x[1][e] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302);
-        x[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
-        x[3][e] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302);
+        if constexpr (F16) {
+          const uint32_t w0 = t.v[2 * e][x] ^ 0x80808080u, w1 = t.v[2 * e + 1][x] ^ 0x80808080u;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) y[b][e] = __builtin_amdgcn_perm(w1, w0, 0x0c040c00 + 0x00010001 * b);
+        } else {
+          uint32_t lo0, hi0, lo1, hi1;
+          codes_bf16<INT8>(t.v[2 * e][x], lo0, hi0);
+          codes_bf16<INT8>(t.v[2 * e + 1][x], lo1, hi1);
+          y[0][e] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100);
+          y[1][e] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302);
+          y[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
+          y[3][e] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302);
+        }
       }
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, u32x4{x[b][0], x[b][1], x[b][2], x[b][3]});
+        const u32x4 vf{y[b][0], y[b][1], y[b][2], y[b][3]};
+        if constexpr (F16) {
+          o[4 * x + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, vf),
+                                                                __builtin_bit_cast(f16x8_t, u32x4{w[0], w[1], w[2], w[3]}),
+                                                                o[4 * x + b], 0, 0, 0);
+        } else {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          o[4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[4 * w + b], 0, 0, 0);
+          for (int n = 0; n < NT; ++n)
+            o[4 * x + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf), pf[n], o[4 * x + b], 0, 0, 0);
+        }
       }
     }
   };
@@ -270,6 +394,15 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
     k += 32 * NW;
   }
   l_run = groups_sum(l_run);
+  if constexpr (F16) {
+    // o = 2^24 (sum of p u) - 128 (sum of p), and from units of 2^M_run to those
+    // of 2^m_run (m_run -inf: the wave had no keys, all zeros)
+    const float bias = 128.f * groups_sum(lp), f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M_run - m_run);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[db][v] = fmaf(o[db][v], 16777216.f, -bias) * f;
+  }
 
   // Merge of the waves.  Lane (c, gq) holds dims (D / 4) gq + DB v + db of head c in o[db][v].
   float* red_m = red;
@@ -303,19 +436,75 @@ __global__ __launch_bounds__(256) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
       acc += f * *reinterpret_cast<const floatx4*>(red_o + (w * nheads + h) * D + d);
     }
     if (part < 0) {
-      acc *= 1.0f / L;
-      T* out = reinterpret_cast<T*>(a.out) + (size_t)row * a.ld_out + (size_t)(head0 + h) * D + d;
-      if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pk_bf16(acc[0], acc[1]), pk_bf16(acc[2], acc[3]));
-      else *reinterpret_cast<floatx4*>(out) = acc;
+      store_out4<T>(a, row, head0 + h, D, d, acc * (1.0f / L));
     } else {
       float* dst = a.part + ((size_t)part * a.nh + head0 + h) * (D + PART_O);
       *reinterpret_cast<floatx4*>(dst + PART_O + d) = acc;
-      if (d == 0) {
-        dst[0] = M;
-        dst[1] = L;
+      if (d == 0) *reinterpret_cast<float2*>(dst) = make_float2(M, L);
+    }
+  }
+}
+
+// The join of the split decodes: one block per (row, head), D / 4 threads per
+// partial row and 256 / (D / 4) of them at once, each thread merging every
+// GR-th split (running maximum, sum and four columns, four splits' loads in
+// flight), then the GR threads of a column in order: the result does not depend
+// on which block finished first.  A launch of its own: counted in by the last
+// block of the row instead, the fence that makes the other blocks' partials
+// visible (one write-back of an XCD's L2 per block) cost 135 us for 640 blocks,
+// this launch 3 to 4.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_join_kernel(Kv8DecodeArgs a) {
+  constexpr int CG = D / 4, GR = 256 / CG, U = 4;
+  __shared__ float jm[GR], jl[GR];
+  __shared__ __align__(16) float jo[GR][D];
+  const int* jn = a.joins + 3 * blockIdx.x;
+  const int row = jn[0], n = jn[1], head = blockIdx.y;
+  const int tid = threadIdx.x, col = tid % CG * 4, g = tid / CG;
+  const float* src = a.part + ((size_t)jn[2] * a.nh + head) * (D + PART_O);
+  const size_t stride = (size_t)a.nh * (D + PART_O);
+  float m = -INFINITY, l = 0.f;
+  floatx4 acc{0.f, 0.f, 0.f, 0.f};
+  for (int j0 = g; j0 < n; j0 += GR * U) {
+    float2 ml[U];
+    floatx4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* p = src + (size_t)min(j0 + u * GR, n - 1) * stride;
+      ml[u] = *reinterpret_cast<const float2*>(p);
+      x[u] = *reinterpret_cast<const floatx4*>(p + PART_O + col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (j0 + u * GR < n) {
+        const float mn = fmaxf(m, ml[u].x), ms = mn == -INFINITY ? 0.f : mn;
+        const float f0 = __builtin_amdgcn_exp2f(m - ms), f1 = __builtin_amdgcn_exp2f(ml[u].x - ms);
+        l = l * f0 + ml[u].y * f1;
+        acc = acc * f0 + x[u] * f1;
+        m = mn;
       }
     }
   }
+  if (col == 0) {
+    jm[g] = m;
+    jl[g] = l;
+  }
+  *reinterpret_cast<floatx4*>(&jo[g][col]) = acc;
+  __syncthreads();
+  if (g > 0) return;
+  float M = jm[0];
+#pragma unroll
+  for (int i = 1; i < GR; ++i) M = fmaxf(M, jm[i]);
+  const float Ms = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  acc = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < GR; ++i) {
+    const float f = __builtin_amdgcn_exp2f(jm[i] - Ms);
+    L = fmaf(f, jl[i], L);
+    acc += f * *reinterpret_cast<const floatx4*>(&jo[i][col]);
+  }
+  store_out4<T>(a, row, head, D, col, acc * (1.0f / L));
 }
 
 template <typename T, int D>
@@ -325,6 +514,7 @@ static hipError_t run_decode(int format, const Kv8DecodeArgs& a, hipStream_t s) 
   const size_t lds = (4 * 32 + (size_t)4 * (group < 16 ? group : 16) * D) * 4;   // at most 33 KB
   if (format == 0) hipLaunchKernelGGL((kv8_attn_rows_kernel<T, D, true>), grid, dim3(256), lds, s, a);
   else hipLaunchKernelGGL((kv8_attn_rows_kernel<T, D, false>), grid, dim3(256), lds, s, a);
+  if (a.n_joins > 0) hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3(a.n_joins, a.nh), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -30,7 +30,7 @@ struct sarathi_kv8_plan {
   int T;
   int n_chunk_units, n_units;    // touched blocks of chunks, then of decodes
   int n_pre, n_dec;              // attention items of chunks and decodes
-  int comb_row0;                 // first row that the combine pass writes (T: none)
+  int comb_row0, comb_rows;      // chunk rows that the combine pass visits: comb_row0 .. comb_rows - 1
   const int* row_slot;           // device
   const int* row_pos;
   const int* comb;
@@ -40,15 +40,17 @@ struct sarathi_kv8_plan {
   const int* dec;
   const float2* tab;
   float* part;
+  const int* joins;
+  int n_joins;
 };
 
 namespace {
 
 // Keys of a decode's work item at least (two steps of each of a block's four
 // waves), and the blocks that the decodes of a batch are split into where their
-// keys allow it (six per CU).
+// keys allow it (three per CU, what runs at once).
 constexpr int DEC_MIN_KEYS = 256, DEC_STEP = 128;
-constexpr long DEC_BLOCKS = 1536;
+constexpr long DEC_BLOCKS = 768;
 // Chunk attention: key tiles of an item at least, the blocks that a batch is
 // split into at most, and the blocks that run at once (two per CU).
 constexpr int PRE_MIN_TILES = 4;
@@ -154,7 +156,7 @@ PlanLayout plan_layout(const sarathi_kv8_cfg& c, int T, int n_chunks) {
   L.tab = take((size_t)T * (c.rope_dim / 2) * sizeof(float2));
   // spans and touched blocks have a row at least
   L.meta_ints = (size_t)T * KV8_SPAN_INTS + (size_t)T * 4 + 4 * (size_t)n_chunks + 4 * (size_t)(qblocks + extra_pre(c)) +
-                5 * (size_t)(T + extra_dec(c));
+                KV8_DEC_INTS * (size_t)(T + extra_dec(c)) + KV8_JOIN_INTS * (size_t)T;
   L.meta = take(L.meta_ints * 4);
   L.part_rows = (size_t)(qblocks + extra_pre(c)) * rpb + T + extra_dec(c);
   L.part = take(L.part_rows * c.n_heads * (c.head_dim + PART_O) * 4);
@@ -164,7 +166,7 @@ PlanLayout plan_layout(const sarathi_kv8_cfg& c, int T, int n_chunks) {
 
 // The batch's work lists and the metadata that goes to the device.
 struct HostPlan {
-  std::vector<int> spans, units, chunks, pre, dec;
+  std::vector<int> spans, units, chunks, pre, dec, joins;
   int n_chunk_units = 0;
   size_t part_rows = 0;
   int comb_row0 = 0;
@@ -245,10 +247,11 @@ void plan_decodes(const sarathi_kv8_cfg& c, const BatchDesc& b, int first_row, H
   const long per_key_range = (long)c.n_kv_heads * head_blocks(c);
   const long target = std::max<long>(DEC_MIN_KEYS, ceil_div(keys * per_key_range, DEC_BLOCKS));
   const int split = ceil_div(target, DEC_STEP) * DEC_STEP;
-  // items run in slot order: the blocks in flight stream the cache in address order
+  // the longest rows first: their blocks start in the first round and short
+  // ones fill the last (48 decodes of 512 to 2048 tokens: 105 us, in slot order 115)
   std::vector<int> order(b.B);
   for (int i = 0; i < b.B; ++i) order[i] = i;
-  std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return b.dslots[x] < b.dslots[y]; });
+  std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return b.dctx[x] > b.dctx[y]; });
   std::vector<int> span(KV8_SPAN_INTS * (size_t)b.B);
   for (int i : order) {
     const int n = b.dctx[i] + 1, want = ceil_div(n, split);
@@ -256,9 +259,12 @@ void plan_decodes(const sarathi_kv8_cfg& c, const BatchDesc& b, int first_row, H
     for (int s = 0; s < ns; ++s)
       p->dec.insert(p->dec.end(), {first_row + i, b.dslots[i], s * len, std::min(n, (s + 1) * len),
                                    ns > 1 ? (int)p->part_rows + s : -1});
-    const int v[KV8_SPAN_INTS] = {b.dslots[i], b.dctx[i], first_row + i, 1, (int)p->part_rows, ns > 1 ? ns : 0, 1};
+    const int v[KV8_SPAN_INTS] = {b.dslots[i], b.dctx[i], first_row + i, 1, 0, 0, 0};   // its own join
     std::copy(v, v + KV8_SPAN_INTS, span.begin() + KV8_SPAN_INTS * (size_t)i);
-    if (ns > 1) p->part_rows += ns;
+    if (ns > 1) {
+      p->joins.insert(p->joins.end(), {first_row + i, ns, (int)p->part_rows});
+      p->part_rows += ns;
+    }
   }
   p->spans.insert(p->spans.end(), span.begin(), span.end());
   for (int i = 0; i < b.B; ++i) {
@@ -275,7 +281,7 @@ int host_plan(const sarathi_kv8_cfg& c, const BatchDesc& b, HostPlan* p) {
   for (size_t i = 0; i < p->spans.size(); i += KV8_SPAN_INTS)
     if (p->spans[i + 5] > 0) p->comb_row0 = std::min(p->comb_row0, p->spans[i + 2]);
   const long T = b.rows(), units = (long)p->units.size() / 4;
-  const long grids[] = {(long)p->pre.size() / 4 * c.n_kv_heads, (long)p->dec.size() / 5 * c.n_kv_heads * head_blocks(c),
+  const long grids[] = {(long)p->pre.size() / 4 * c.n_kv_heads, (long)p->dec.size() / KV8_DEC_INTS * c.n_kv_heads * head_blocks(c),
                         T * ((c.n_heads + 7) / 8) + units * 2 * c.n_kv_heads, T * 2 * c.n_kv_heads * (c.head_dim / 16) / 256 + 1};
   for (long g : grids)
     if (g > MAX_GRID) return fail(SARATHI_EUNSUPPORTED, "batch of %ld rows x %d heads needs more than %ld blocks", T, c.n_heads, MAX_GRID);
@@ -326,7 +332,8 @@ int plan_upload(const sarathi_kv8* kv, const BatchDesc& b, void* ws, size_t ws_b
   if (rc) return rc;
   std::vector<int> meta;
   auto put = [&](const std::vector<int>& v) { const size_t at = meta.size(); meta.insert(meta.end(), v.begin(), v.end()); return at; };
-  const size_t o_spans = put(h.spans), o_units = put(h.units), o_chunks = put(h.chunks), o_pre = put(h.pre), o_dec = put(h.dec);
+  const size_t o_spans = put(h.spans), o_units = put(h.units), o_chunks = put(h.chunks), o_pre = put(h.pre), o_dec = put(h.dec),
+               o_joins = put(h.joins);
   if (meta.size() > L.meta_ints || h.part_rows > L.part_rows)   // the bounds hold for every checked batch
     return fail(SARATHI_EINVAL, "internal: batch plan exceeds its workspace layout");
   char* base = static_cast<char*>(ws);
@@ -335,12 +342,13 @@ int plan_upload(const sarathi_kv8* kv, const BatchDesc& b, void* ws, size_t ws_b
   plan->cfg = c; plan->mem = kv->mem; plan->st = kv->st;
   plan->T = T;
   plan->n_chunk_units = h.n_chunk_units; plan->n_units = (int)h.units.size() / 4;
-  plan->n_pre = (int)h.pre.size() / 4; plan->n_dec = (int)h.dec.size() / 5;
-  plan->comb_row0 = h.comb_row0;
+  plan->n_pre = (int)h.pre.size() / 4; plan->n_dec = (int)h.dec.size() / KV8_DEC_INTS;
+  plan->comb_row0 = h.comb_row0; plan->comb_rows = T - b.B;
   plan->row_slot = rows; plan->row_pos = rows + T; plan->comb = rows + 2 * (size_t)T;
   plan->units = dm + o_units; plan->chunks = dm + o_chunks; plan->pre = dm + o_pre; plan->dec = dm + o_dec;
   plan->tab = reinterpret_cast<float2*>(base + L.tab);
   plan->part = reinterpret_cast<float*>(base + L.part);
+  plan->joins = dm + o_joins; plan->n_joins = (int)h.joins.size() / KV8_JOIN_INTS;
   MetaChunk mc;
   for (size_t at = 0; at < meta.size(); at += META_CHUNK) {
     mc.count = (int)std::min<size_t>(META_CHUNK, meta.size() - at);
@@ -385,12 +393,13 @@ int run_attention(const sarathi_kv8_plan* p, int layer, const void* q, size_t ld
   if (p->n_dec > 0) {
     Kv8DecodeArgs a{};
     a.q = q; a.ld_q = ld_q; a.out = out; a.ld_out = ld_out; a.work = p->dec; a.n_work = p->n_dec;
-    a.nh = c.n_heads; a.nkv = c.n_kv_heads; a.part = p->part; a.scale_log2 = scale_log2; a.kv = layer_of(p, layer);
+    a.nh = c.n_heads; a.nkv = c.n_kv_heads; a.part = p->part; a.joins = p->joins; a.n_joins = p->n_joins; a.scale_log2 = scale_log2;
+    a.kv = layer_of(p, layer);
     e = launch_kv8_decode(c.dtype, c.format, c.head_dim, a, s);
     if (e != hipSuccess) return hip_fail(e, "decode attention");
   }
   CombineArgs ca{};
-  ca.part = p->part; ca.comb = p->comb; ca.row0 = p->comb_row0; ca.n_rows = p->T; ca.nh = c.n_heads; ca.hd = c.head_dim;
+  ca.part = p->part; ca.comb = p->comb; ca.row0 = p->comb_row0; ca.n_rows = p->comb_rows; ca.nh = c.n_heads; ca.hd = c.head_dim;
   ca.out = out; ca.ld_out = (int)ld_out;
   e = launch_attn_combine(c.dtype, ca, s);
   return e == hipSuccess ? SARATHI_OK : hip_fail(e, "attention combine");
