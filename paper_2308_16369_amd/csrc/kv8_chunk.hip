@@ -85,7 +85,7 @@ __device__ __forceinline__ uint2 lds_tr16(const char* p) {
 }
 
 template <typename T, int D, bool INT8>
-__global__ __launch_bounds__(256) void kv8_attn_chunk_kernel(Kv8ChunkArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_kernel(Kv8ChunkArgs a) {
   constexpr int NT = sizeof(T) == 2 ? 1 : 3;
   constexpr int KT = KV8_KT, QB = KV8_QB;
   constexpr int DCH = D / 8;             // 16-byte chunks per bf16 tile row
