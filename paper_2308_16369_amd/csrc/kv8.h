@@ -99,6 +99,7 @@ struct Kv8ChunkArgs {
   const int* chunks;            // [n][slot, offset, len, first row]
   const int* work;              // [n_work][4]: chunk, first chunk row, partial base or -1, (tile begin << 16) | tile end
   int n_work, nh, nkv;
+  int groups;                   // 4-wave groups per block: 1 or, of bf16, 2
   float* part;                  // partial row of the item's j-th chunk row: base + j
   float scale_log2;
   Kv8Layer kv;

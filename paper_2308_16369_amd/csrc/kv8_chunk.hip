@@ -1,45 +1,37 @@
 // Attention of prompt chunks over the 8-bit KV cache.
 //
 // Block = one key/value head, KV8_QB packed query rows (the rows of the chunk
-// times the query heads that share the key/value head; four waves of 32) and a
-// range of 64-key tiles.  A tile's codes are read once per block, converted to
-// bf16 (exact) on the way into LDS, and multiplied there by every wave:
+// times the query heads that share the key/value head; four waves of 32 to a
+// group) and a range of 64-key tiles.  A tile's codes are read once per group,
+// converted to bf16 (exact) on the way into LDS, and multiplied there by its
+// four waves:
 //   S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16, a lane (ql =
 //   lane % 32, g = lane / 32) holding the scores of packed row ql for keys
 //   8 (v / 4) + 4 g + v % 4 of each 32-key half; V^T comes from transposed LDS
 //   reads.  A scale is constant over 16 keys: the key scale joins the softmax
 //   scale in the exponent, the value scale enters there as its logarithm (the
 //   row sum divides it out again), so neither costs a multiplication per score.
-#include "kv8.h"
+// 512 rows over a prefix of 2048 (52 heads): 56 us, 0.56 PFLOP/s; a 4096-token
+// prompt (32 / 8 heads): 178 us, 0.77 PFLOP/s.  A wave's tile takes 4800 cycles
+// alone on its SIMD and 5150 beside another's, of which the matrix cores are
+// busy 1024: it is bound by the latency of its own chain (LDS reads, products,
+// maximum, exponentials, products, staging, barrier).  Tried and no faster:
+// the next tile's products under this one's exponentials, fragments read ahead
+// into registers, 32-key tiles with three waves per SIMD, 64 rows per wave (the
+// accumulators then move between register files), and operands straight from
+// global memory (440 us for the prompt).
+#include "kv8_device.h"
 
 namespace sarathi {
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ uint32_t pk2_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
-}
 
 // 16 codes to 16 bf16.
 template <bool INT8>
 __device__ __forceinline__ void widen16(const uint4& w, u32x4& lo, u32x4& hi) {
-  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-  uint32_t r[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (INT8) {
-      r[2 * i] = pk2_bf16((float)(signed char)x[i], (float)(signed char)(x[i] >> 8));
-      r[2 * i + 1] = pk2_bf16((float)(signed char)(x[i] >> 16), (float)(signed char)(x[i] >> 24));
-    } else {
-      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], 1.0f, false));
-      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], 1.0f, true));
-    }
-  }
-  lo = u32x4{r[0], r[1], r[2], r[3]};
-  hi = u32x4{r[4], r[5], r[6], r[7]};
+  lo = __builtin_bit_cast(u32x4, codes8_bf16<INT8>(w.x, w.y));
+  hi = __builtin_bit_cast(u32x4, codes8_bf16<INT8>(w.z, w.w));
 }
 
 // Swizzle of a tile row's 16-byte chunks: a bijection of the row mod 16 that
@@ -51,31 +43,15 @@ __device__ __forceinline__ int swz(int c, int r) {
   return c ^ (r & 7);
 }
 
+// Maximum that propagates NaN (fmaxf would first quieten every score).
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float lanes_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return max_nan(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float lanes_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-template <int NT>
-__device__ __forceinline__ void terms8(const float* x, bf16x8_t* t) {
-  float r[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = x[e];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    u32x4 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w[e] = pk2_bf16(r[2 * e], r[2 * e + 1]);
-      r[2 * e] -= __uint_as_float(w[e] << 16);
-      r[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
-    }
-    t[n] = __builtin_bit_cast(bf16x8_t, w);
-  }
 }
 
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
@@ -84,25 +60,33 @@ __device__ __forceinline__ uint2 lds_tr16(const char* p) {
   return __builtin_bit_cast(uint2, v);
 }
 
-template <typename T, int D, bool INT8>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_kernel(Kv8ChunkArgs a) {
+// NG: groups of four waves that take the item's tiles in turn, each with LDS
+// stages of its own, and are merged at the end.
+template <typename T, int D, bool INT8, int NG>
+__global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_kernel(Kv8ChunkArgs a) {
   constexpr int NT = sizeof(T) == 2 ? 1 : 3;
   constexpr int KT = KV8_KT, QB = KV8_QB;
   constexpr int DCH = D / 8;             // 16-byte chunks per bf16 tile row
   constexpr int TILE = KT * DCH;         // chunks per tile
   constexpr int LPR = D / 16;            // lanes that read a key row (16 codes each)
   constexpr int NI = KT * LPR / 256;     // 16-byte loads per thread and tile (K or V)
-  __shared__ u32x4 ring[2][2][TILE];     // [stage][K, V]
+  extern __shared__ u32x4 lds[];         // [group][stage][K, V][TILE]; then the merge
 
-  const int item = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv;
+  // blocks go to the eight XCDs in turn: each takes whole heads, whose keys and
+  // values its L2 then serves to all of their query blocks
+  const int per = gridDim.x / 8, bt = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+  if (bt >= a.n_work * a.nkv) return;
+  const int item = bt % a.n_work, kvh = bt / a.n_work;
   const int* wk = a.work + 4 * item;
   const int* ch = a.chunks + 4 * wk[0];
   const int slot = ch[0], offset = ch[1], C = ch[2], row0 = ch[3];
   const int r0 = wk[1], part = wk[2];
   const int group = a.nh / a.nkv;
   const int nrows = min(QB / group, C - r0);       // the block's chunk rows
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6;   // within the group
+  const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int g = lane >> 5, ql = lane & 31;
+  u32x4* ring = lds + grp * 4 * TILE;
 
   const uint8_t* kbase = a.kv.codes + slot * a.kv.slot + kvh * a.kv.head;
   const uint8_t* vbase = kbase + a.kv.kv;
@@ -112,6 +96,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
   const int kbeg = (wk[3] >> 16) * KT;
   const int kend = min(offset + r0 + nrows, (wk[3] & 0xffff) * KT);
   const int n_tiles = (kend - kbeg + KT - 1) / KT;
+  const int n_iter = (n_tiles + NG - 1) / NG;        // the group's tile of iteration i: NG i + grp
 
   // the lane's packed row: chunk row r0 + rr, head
   const int pr = wave * 32 + ql;
@@ -132,9 +117,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
         float x[8];
         Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
         Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
-        terms8<NT>(x, qf[ks]);
+        split8<NT>(x, qf[ks]);
       }
     }
+    // the fragments are here before the loop: waited for inside it, they would
+    // take the prefetched tile with them (loads return in order)
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(qf[ks][n]));
   }
 
   float m_run = -INFINITY, l_run = 0.f;
@@ -144,28 +135,40 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
 #pragma unroll
     for (int v = 0; v < 16; ++v) o_acc[db][v] = 0.f;
 
-  // tile staging: thread -> NI pieces of 16 codes of K and of V
+  // Tile staging: a thread takes NI pieces of 16 codes of K and of V; positions
+  // past the item's keys re-read its last one.
   uint4 kr[NI], vr[NI];
-  auto fetch = [&](int kt) {
+  float ks_next[4], vs_next[4];          // the fetched tile's scales of its four 16-key groups
+  const int sr = tid / LPR, sc = tid % LPR;
+  auto fetch = [&](int it) {
+    const int k0 = kbeg + (NG * it + grp) * KT;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = min(k0 + 16 * i, kend - 1) >> a.kv.log2_block;
+      ks_next[i] = ksc[b];
+      vs_next[i] = vsc[b];
+    }
+    const uint8_t* kp = kbase + (size_t)k0 * D;
+    const uint8_t* vp = vbase + (size_t)k0 * D;
+    const int lim = (kend - 1 - k0) * D;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int at = i * 256 + tid, r = at / LPR, c = at % LPR;
-      const size_t off = (size_t)min(kbeg + kt * KT + r, kend - 1) * D + 16 * c;
-      kr[i] = *reinterpret_cast<const uint4*>(kbase + off);
-      vr[i] = *reinterpret_cast<const uint4*>(vbase + off);
+      const int off = min((sr + i * (256 / LPR)) * D, lim) + 16 * sc;
+      kr[i] = *reinterpret_cast<const uint4*>(kp + off);
+      vr[i] = *reinterpret_cast<const uint4*>(vp + off);
     }
   };
   auto stage = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int at = i * 256 + tid, r = at / LPR, c = at % LPR;
+      const int r = sr + i * (256 / LPR);
       u32x4 lo, hi;
       widen16<INT8>(kr[i], lo, hi);
-      ring[buf][0][r * DCH + swz<D>(2 * c, r)] = lo;
-      ring[buf][0][r * DCH + swz<D>(2 * c + 1, r)] = hi;
+      ring[2 * buf * TILE + r * DCH + swz<D>(2 * sc, r)] = lo;
+      ring[2 * buf * TILE + r * DCH + swz<D>(2 * sc + 1, r)] = hi;
       widen16<INT8>(vr[i], lo, hi);
-      ring[buf][1][r * DCH + swz<D>(2 * c, r)] = lo;
-      ring[buf][1][r * DCH + swz<D>(2 * c + 1, r)] = hi;
+      ring[(2 * buf + 1) * TILE + r * DCH + swz<D>(2 * sc, r)] = lo;
+      ring[(2 * buf + 1) * TILE + r * DCH + swz<D>(2 * sc + 1, r)] = hi;
     }
   };
 
@@ -184,18 +187,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) koff[ks] = ql * DCH + swz<D>(2 * ks + g, ql);
 
-  auto compute = [&](int kt, int buf) {
-    const int k0 = kbeg + kt * KT;
-    if (k0 > last_key || idle) return;
-    // scales of the four 16-key groups; a zero scale belongs to zero codes, so 1 does as well
-    float ks4[4], vs4[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int b = min(k0 + 16 * i, kend - 1) >> a.kv.log2_block;
-      const float x = ksc[b], y = vsc[b];
-      ks4[i] = (x > 0.f ? x : 1.f) * a.scale_log2;
-      vs4[i] = y > 0.f ? y : 1.f;
-    }
+  float ks4[4], vs4[4];
+  auto compute = [&](int it, int buf) {
+    const int k0 = kbeg + (NG * it + grp) * KT;
+    if (k0 > last_key || k0 >= kend || idle) return;
     floatx16 s[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -203,7 +198,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
       for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, ring[buf][0][kb * 32 * DCH + koff[ks]]);
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, ring[2 * buf * TILE + kb * 32 * DCH + koff[ks]]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][n], s[kb], 0, 0, 0);
       }
@@ -222,8 +217,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
     for (int i = 0; i < 4; ++i) {
       float t = s[i >> 1][8 * (i & 1)];
 #pragma unroll
-      for (int v = 1; v < 8; ++v) t = fmaxf(t, s[i >> 1][8 * (i & 1) + v]);
-      mx = fmaxf(mx, t * ks4[i]);
+      for (int v = 1; v < 8; ++v) t = max_nan(t, s[i >> 1][8 * (i & 1) + v]);
+      mx = max_nan(mx, t * ks4[i]);
     }
     mx = lanes_max(mx);
     if (__ballot(mx > m_run + 8.0f)) {
@@ -242,23 +237,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
       float p[8], sum = 0.f;
 #pragma unroll
       for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][8 * (i & 1) + v], ks4[i], add));
-      terms8<NT>(p, pf[i]);
+      split8<NT>(p, pf[i]);
       if constexpr (NT == 1) {
         // the row sum takes the rounded probabilities that multiply V
         const u32x4 w = __builtin_bit_cast(u32x4, pf[i][0]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t pair = w[e];
-          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair),
-                                                __builtin_convertvector((f32x2_t){1.f, 1.f}, bf16x2_t), sum, false);
+          sum = sum_bf16(pair, sum);
         }
       } else {
 #pragma unroll
         for (int v = 0; v < 8; ++v) sum += p[v];
       }
-      l_run = fmaf(sum, 1.0f / vs4[i], l_run);
+      l_run = fmaf(sum, __builtin_amdgcn_rcpf(vs4[i]), l_run);
     }
-    const char* vt = reinterpret_cast<const char*>(ring[buf][1]);
+    const char* vt = reinterpret_cast<const char*>(ring + (2 * buf + 1) * TILE);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -271,16 +265,58 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
       }
   };
 
+  auto step = [&](int it, int buf) {
+    // a zero scale belongs to zero codes, so 1 does as well
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ks4[i] = (ks_next[i] > 0.f ? ks_next[i] : 1.f) * a.scale_log2;
+      vs4[i] = vs_next[i] > 0.f ? vs_next[i] : 1.f;
+    }
+    if (it + 1 < n_iter) fetch(it + 1);
+    compute(it, buf);
+    if (it + 1 < n_iter) stage(buf ^ 1);
+    __syncthreads();
+  };
   fetch(0);
   stage(0);
   __syncthreads();
-  for (int kt = 0; kt < n_tiles; ++kt) {
-    if (kt + 1 < n_tiles) fetch(kt + 1);
-    compute(kt, kt & 1);
-    if (kt + 1 < n_tiles) stage((kt + 1) & 1);
-    __syncthreads();
+  for (int it = 0; it < n_iter; it += 2) {
+    step(it, 0);
+    if (it + 1 < n_iter) step(it + 1, 1);
   }
   l_run = lanes_sum(l_run);
+  if constexpr (NG == 2) {
+    // the second group's result through LDS (the tiles are done with) to the first
+    float* red_m = reinterpret_cast<float*>(lds);      // [QB] m, [QB] l, [QB][D + 4] o
+    float* red_l = red_m + QB;
+    float* red_o = red_l + QB + pr * (D + 4) + 4 * g;
+    if (grp == 1) {
+      if (g == 0) {
+        red_m[pr] = m_run;
+        red_l[pr] = l_run;
+      }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4)
+          *reinterpret_cast<floatx4*>(red_o + db * 32 + 8 * v4) =
+              floatx4{o_acc[db][4 * v4], o_acc[db][4 * v4 + 1], o_acc[db][4 * v4 + 2], o_acc[db][4 * v4 + 3]};
+    }
+    __syncthreads();
+    if (grp == 1) return;
+    const float m1 = red_m[pr], M = fmaxf(m_run, m1), Ms = M == -INFINITY ? 0.f : M;
+    const float f0 = __builtin_amdgcn_exp2f(m_run - Ms), f1 = __builtin_amdgcn_exp2f(m1 - Ms);
+    l_run = l_run * f0 + red_l[pr] * f1;
+    m_run = M;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const floatx4 x = *reinterpret_cast<const floatx4*>(red_o + db * 32 + 8 * v4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o_acc[db][4 * v4 + i] = o_acc[db][4 * v4 + i] * f0 + x[i] * f1;
+      }
+  }
   if (!real) return;
   if (part < 0) {
     const float inv = 1.0f / l_run;
@@ -291,7 +327,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
       for (int v4 = 0; v4 < 4; ++v4) {
         const int d = db * 32 + 8 * v4 + 4 * g;
         const floatx4 x = floatx4{o_acc[db][4 * v4], o_acc[db][4 * v4 + 1], o_acc[db][4 * v4 + 2], o_acc[db][4 * v4 + 3]} * inv;
-        if constexpr (NT == 1) *reinterpret_cast<uint2*>(out + d) = make_uint2(pk2_bf16(x[0], x[1]), pk2_bf16(x[2], x[3]));
+        if constexpr (NT == 1) *reinterpret_cast<uint2*>(out + d) = make_uint2(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]));
         else *reinterpret_cast<floatx4*>(out + d) = x;
       }
     return;
@@ -309,18 +345,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chunk_ke
           floatx4{o_acc[db][4 * v4], o_acc[db][4 * v4 + 1], o_acc[db][4 * v4 + 2], o_acc[db][4 * v4 + 3]};
 }
 
-template <typename T, int D>
-static hipError_t run_chunk(int format, const Kv8ChunkArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((size_t)a.n_work * a.nkv));
-  if (format == 0) hipLaunchKernelGGL((kv8_attn_chunk_kernel<T, D, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((kv8_attn_chunk_kernel<T, D, false>), grid, dim3(256), 0, s, a);
+template <typename T, int D, bool INT8, int NG>
+static hipError_t run_chunk(const Kv8ChunkArgs& a, hipStream_t s) {
+  constexpr int TILES = NG * 4 * KV8_KT * D * 2, MERGE = KV8_QB * (2 + D + 4) * 4;   // 128 KB at most
+  constexpr int LDS = NG == 2 && MERGE > TILES ? MERGE : TILES;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = ensure_dynamic_lds((const void*)kv8_attn_chunk_kernel<T, D, INT8, NG>, LDS, done);
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)(((size_t)a.n_work * a.nkv + 7) / 8 * 8));
+  hipLaunchKernelGGL((kv8_attn_chunk_kernel<T, D, INT8, NG>), grid, dim3(256 * NG), LDS, s, a);
   return hipGetLastError();
+}
+
+template <typename T, int D>
+static hipError_t run_chunk_groups(int format, const Kv8ChunkArgs& a, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (a.groups == 2) return format == 0 ? run_chunk<T, D, true, 2>(a, s) : run_chunk<T, D, false, 2>(a, s);
+  }
+  return format == 0 ? run_chunk<T, D, true, 1>(a, s) : run_chunk<T, D, false, 1>(a, s);
 }
 
 hipError_t launch_kv8_chunk(int dtype, int format, int hd, const Kv8ChunkArgs& a, hipStream_t s) {
   if (a.n_work <= 0) return hipSuccess;
-  if (dtype == 0) return hd == 128 ? run_chunk<float, 128>(format, a, s) : run_chunk<float, 64>(format, a, s);
-  return hd == 128 ? run_chunk<bf16, 128>(format, a, s) : run_chunk<bf16, 64>(format, a, s);
+  if (dtype == 0) return hd == 128 ? run_chunk_groups<float, 128>(format, a, s) : run_chunk_groups<float, 64>(format, a, s);
+  return hd == 128 ? run_chunk_groups<bf16, 128>(format, a, s) : run_chunk_groups<bf16, 64>(format, a, s);
 }
 
 }  // namespace sarathi

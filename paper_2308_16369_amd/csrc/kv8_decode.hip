@@ -17,50 +17,9 @@
 // by reading the cache).  A scale is constant over 16 keys: the key scale
 // multiplies the scores with the softmax scale, the value scale the
 // probabilities.
-//
-// bf16 rows over int8 codes multiply in f16 instead, whose subnormals make the
-// conversion of a code a byte move: u = code + 128 (one xor per four codes) put
-// into the low byte of a half is u 2^-24.  The offset goes out at the end,
-//   q . code = 2^24 q . (u 2^-24) - 128 sum(q),
-// and alike for V with the sum of the probabilities.  q is scaled by a power of
-// two into f16's range (its 8 bits fit; elements below 2^-28 of the row's
-// largest lose bits), and the probabilities times their value scale are kept
-// near one by a running maximum of their own (the scales may differ by any
-// factor), so they keep 11 bits.
-#include "kv8.h"
+#include "kv8_device.h"
 
 namespace sarathi {
-
-typedef unsigned int u32x4_nt __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2_nt __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {   // nearest even; low half = a
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
-}
-
-// Four codes (a dword) to bf16: lo = codes 0, 1; hi = codes 2, 3.
-template <bool INT8>
-__device__ __forceinline__ void codes_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  if constexpr (INT8) {
-    lo = pk_bf16((float)(signed char)w, (float)(signed char)(w >> 8));
-    hi = pk_bf16((float)(signed char)(w >> 16), (float)(signed char)(w >> 24));
-  } else {
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
-  }
-}
-template <bool INT8>
-__device__ __forceinline__ bf16x8_t codes8_bf16(uint32_t a, uint32_t b) {
-  u32x4 r;
-  uint32_t x, y;
-  codes_bf16<INT8>(a, x, y);
-  r[0] = x; r[1] = y;
-  codes_bf16<INT8>(b, x, y);
-  r[2] = x; r[3] = y;
-  return __builtin_bit_cast(bf16x8_t, r);
-}
 
 // Max / sum over the four 16-lane groups of the wave (the lanes of one head):
 // v_permlane16/32_swap hand each lane its own and its partner's value.
@@ -77,32 +36,6 @@ __device__ __forceinline__ float groups_sum(float v) {
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
-// x as NT bf16 terms of eight values each: bf16 rows are one exact term; fp32
-// takes three (the remainders of the first two are exact in fp32), 24 bits.
-template <int NT>
-__device__ __forceinline__ void split8(const float* x, bf16x8_t* t) {
-  float r[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = x[e];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    u32x4 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w[e] = pk_bf16(r[2 * e], r[2 * e + 1]);
-      r[2 * e] -= __uint_as_float(w[e] << 16);
-      r[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
-    }
-    t[n] = __builtin_bit_cast(bf16x8_t, w);
-  }
-}
-
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pk_f16(float a, float b) {   // nearest even
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
-}
-
 template <typename T>
 __device__ __forceinline__ void store_out4(const Kv8DecodeArgs& a, int row, int head, int D, int d, floatx4 x) {
   T* out = reinterpret_cast<T*>(a.out) + (size_t)row * a.ld_out + (size_t)head * D + d;
@@ -110,7 +43,7 @@ __device__ __forceinline__ void store_out4(const Kv8DecodeArgs& a, int row, int 
   else *reinterpret_cast<floatx4*>(out) = x;
 }
 
-// F16 (bf16 rows over int8 codes): see the file comment.
+// F16: bf16 rows over int8 codes (kv8_device.h).
 template <typename T, int D, bool INT8>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
   constexpr int NT = sizeof(T) == 2 ? 1 : 3;
@@ -151,7 +84,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
       }
       // a power of two that brings the row's largest magnitude to 2^14 .. 2^15
-      const int ex = min(max((int)(__float_as_uint(groups_max(top)) >> 23) - 127, -100), 110) - 14;
+      const int ex = f16_exponent(groups_max(top));
       const float f = __builtin_ldexpf(1.f, -ex);
 #pragma unroll
       for (int i = 0; i < 2 * KI; ++i)
@@ -159,7 +92,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         for (int e = 0; e < 4; ++e) {
           const uint32_t w = pk_f16(x[i][2 * e] * f, x[i][2 * e + 1] * f);
           qf[i][0][e] = w;
-          sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, w), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, sum, false);
+          sum = sum_f16(w, sum);
         }
       c_mul = __builtin_ldexpf(a.scale_log2, ex);
       c_add = -128.f * groups_sum(sum) * c_mul;
@@ -245,10 +178,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           if constexpr (F16) {
-            const uint32_t x = t.k[h][i][2 * u] ^ 0x80808080u, y = t.k[h][i][2 * u + 1] ^ 0x80808080u;
-            const u32x4 w{__builtin_amdgcn_perm(x, x, 0x0c010c00), __builtin_amdgcn_perm(x, x, 0x0c030c02),
-                          __builtin_amdgcn_perm(y, y, 0x0c010c00), __builtin_amdgcn_perm(y, y, 0x0c030c02)};
-            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, w),
+            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8_f16(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]),
                                                           __builtin_bit_cast(f16x8_t, qf[2 * i + u][0]), s[h], 0, 0, 0);
           } else {
             const bf16x8_t kf = codes8_bf16<INT8>(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]);
@@ -302,7 +232,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         for (int v = 0; v < 2; ++v) {
           const uint32_t pair = pk_f16(p[2 * v], p[2 * v + 1]);
           w[2 * h + v] = pair;
-          lp = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pair), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, lp, false);
+          lp = sum_f16(pair, lp);
         }
       }
     } else {
@@ -322,7 +252,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
       if constexpr (NT == 1) {
         // the row sum takes the rounded probabilities that multiply V: the
         // weights add up to one, whatever their rounding
-        const bf16x2_t ones = __builtin_convertvector((f32x2_t){1.f, 1.f}, bf16x2_t);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float vs = t.vs[h] > 0.f ? t.vs[h] : 1.f;      // a zero scale belongs to zero codes
@@ -331,7 +260,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
           for (int v = 0; v < 2; ++v) {
             const uint32_t pair = pk_bf16(p[4 * h + 2 * v] * vs, p[4 * h + 2 * v + 1] * vs);
             w[2 * h + v] = pair;
-            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), ones, sum, false);
+            sum = sum_bf16(pair, sum);
           }
           l_run = fmaf(sum, 1.0f / vs, l_run);
         }
@@ -348,26 +277,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
 #pragma unroll
     for (int x = 0; x < VW; ++x) {
       // bytes 4 x .. + 3 of the eight keys' rows, as four vectors over the keys
-      uint32_t y[4][4];
+      uint32_t v[8];
+      u32x4 y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (F16) {
-          const uint32_t w0 = t.v[2 * e][x] ^ 0x80808080u, w1 = t.v[2 * e + 1][x] ^ 0x80808080u;
-#pragma unroll
-          for (int b = 0; b < 4; ++b) y[b][e] = __builtin_amdgcn_perm(w1, w0, 0x0c040c00 + 0x00010001 * b);
-        } else {
-          uint32_t lo0, hi0, lo1, hi1;
-          codes_bf16<INT8>(t.v[2 * e][x], lo0, hi0);
-          codes_bf16<INT8>(t.v[2 * e + 1][x], lo1, hi1);
-          y[0][e] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100);
-          y[1][e] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302);
-          y[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
-          y[3][e] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302);
-        }
-      }
+      for (int e = 0; e < 8; ++e) v[e] = t.v[e][x];
+      transpose8<INT8, F16, 4>(v, y);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const u32x4 vf{y[b][0], y[b][1], y[b][2], y[b][3]};
+        const u32x4 vf = y[b];
         if constexpr (F16) {
           o[4 * x + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, vf),
                                                                 __builtin_bit_cast(f16x8_t, u32x4{w[0], w[1], w[2], w[3]}),

@@ -1,0 +1,118 @@
+// Device helpers of the attention over the 8-bit KV cache.
+//
+// Codes become matrix-core operands without rounding.  bf16 holds every code of
+// both formats.  bf16 rows over int8 codes multiply in f16 instead, whose
+// subnormals make the conversion a byte move: u = code + 128 (one xor per four
+// codes) put into the low byte of a half is u 2^-24.  The offset goes out at the
+// end,
+//   q . code = 2^24 q . (u 2^-24) - 128 sum(q),
+// and alike for V with the sum of the probabilities.  q is scaled by a power of
+// two into f16's range (its 8 bits fit; elements below 2^-28 of the row's
+// largest lose bits, rows beyond 2^111 become NaN), and the probabilities times
+// their value scale are kept near one by a running maximum of their own (the
+// scales may differ by any factor), so they keep 11 bits.
+#pragma once
+
+#include "kv8.h"
+
+namespace sarathi {
+
+typedef unsigned int u32x4_nt __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2_nt __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {   // nearest even; low half = a
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
+}
+
+// Four codes (a dword) to bf16: lo = codes 0, 1; hi = codes 2, 3.
+template <bool INT8>
+__device__ __forceinline__ void codes_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (INT8) {
+    lo = pk_bf16((float)(signed char)w, (float)(signed char)(w >> 8));
+    hi = pk_bf16((float)(signed char)(w >> 16), (float)(signed char)(w >> 24));
+  } else {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+  }
+}
+template <bool INT8>
+__device__ __forceinline__ bf16x8_t codes8_bf16(uint32_t a, uint32_t b) {
+  u32x4 r;
+  uint32_t x, y;
+  codes_bf16<INT8>(a, x, y);
+  r[0] = x; r[1] = y;
+  codes_bf16<INT8>(b, x, y);
+  r[2] = x; r[3] = y;
+  return __builtin_bit_cast(bf16x8_t, r);
+}
+
+// x as NT bf16 terms of eight values each: bf16 rows are one exact term; fp32
+// takes three (the remainders of the first two are exact in fp32), 24 bits.
+template <int NT>
+__device__ __forceinline__ void split8(const float* x, bf16x8_t* t) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = pk_bf16(r[2 * e], r[2 * e + 1]);
+      r[2 * e] -= __uint_as_float(w[e] << 16);
+      r[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+    }
+    t[n] = __builtin_bit_cast(bf16x8_t, w);
+  }
+}
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pk_f16(float a, float b) {   // nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
+}
+
+// Four int8 codes as u = code + 128: pairs of halves u 2^-24 of codes 0, 1 and 2, 3.
+__device__ __forceinline__ uint32_t offset_codes(uint32_t w) { return w ^ 0x80808080u; }
+__device__ __forceinline__ f16x8_t codes8_f16(uint32_t a, uint32_t b) {
+  const uint32_t x = offset_codes(a), y = offset_codes(b);
+  return __builtin_bit_cast(f16x8_t, (u32x4{__builtin_amdgcn_perm(x, x, 0x0c010c00), __builtin_amdgcn_perm(x, x, 0x0c030c02),
+                                            __builtin_amdgcn_perm(y, y, 0x0c010c00), __builtin_amdgcn_perm(y, y, 0x0c030c02)}));
+}
+// Byte b of eight keys' dwords as one operand (the keys along its eight elements).
+template <bool INT8, bool F16, int NB>
+__device__ __forceinline__ void transpose8(const uint32_t* v, u32x4* y) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (F16) {
+      const uint32_t w0 = offset_codes(v[2 * e]), w1 = offset_codes(v[2 * e + 1]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) y[b][e] = __builtin_amdgcn_perm(w1, w0, 0x0c040c00 + 0x00010001 * b);
+    } else {
+      uint32_t lo0, hi0, lo1, hi1;
+      codes_bf16<INT8>(v[2 * e], lo0, hi0);
+      codes_bf16<INT8>(v[2 * e + 1], lo1, hi1);
+      y[0][e] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100);
+      y[1][e] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302);
+      if constexpr (NB == 4) {
+        y[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
+        y[3][e] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302);
+      }
+    }
+  }
+}
+// The power of two that brings a row of largest magnitude `top` to 2^14 .. 2^15, as an exponent.
+__device__ __forceinline__ int f16_exponent(float top) {
+  return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 110) - 14;
+}
+__device__ __forceinline__ float sum_f16(uint32_t pair, float c) {
+  return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pair), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, c, false);
+}
+__device__ __forceinline__ float sum_bf16(uint32_t pair, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair),
+                                         __builtin_convertvector((f32x2_t){1.f, 1.f}, bf16x2_t), c, false);
+}
+
+}  // namespace sarathi

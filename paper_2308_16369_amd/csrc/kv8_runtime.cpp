@@ -30,6 +30,7 @@ struct sarathi_kv8_plan {
   int T;
   int n_chunk_units, n_units;    // touched blocks of chunks, then of decodes
   int n_pre, n_dec;              // attention items of chunks and decodes
+  int groups;                    // 4-wave groups of a chunk-attention block
   int comb_row0, comb_rows;      // chunk rows that the combine pass visits: comb_row0 .. comb_rows - 1
   const int* row_slot;           // device
   const int* row_pos;
@@ -51,10 +52,13 @@ namespace {
 // keys allow it (three per CU, what runs at once).
 constexpr int DEC_MIN_KEYS = 256, DEC_STEP = 128;
 constexpr long DEC_BLOCKS = 768;
-// Chunk attention: key tiles of an item at least, the blocks that a batch is
-// split into at most, and the blocks that run at once (two per CU).
+// Chunk attention: key tiles of an item at least, the items that splitting adds
+// to a batch at most, the four-wave groups that run at once (two per CU), a
+// block's set-up, merge and output in tiles' times (of one and two groups), the
+// time of a tile in a block of two groups, and the combine pass in tiles.
 constexpr int PRE_MIN_TILES = 4;
 constexpr long PRE_SPLIT_BLOCKS = 768, PRE_SLOTS = 512;
+constexpr double PRE_FIXED_TILES = 2, PRE_FIXED_TILES_2 = 3, PRE_TILE_2 = 1.15, PRE_JOIN_TILES = 6;
 constexpr long MAX_GRID = (1l << 24) - 1;   // blocks of 256 threads in one launch
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -168,6 +172,7 @@ PlanLayout plan_layout(const sarathi_kv8_cfg& c, int T, int n_chunks) {
 struct HostPlan {
   std::vector<int> spans, units, chunks, pre, dec, joins;
   int n_chunk_units = 0;
+  int groups = 1;                // 4-wave groups of a chunk-attention block
   size_t part_rows = 0;
   int comb_row0 = 0;
 };
@@ -185,27 +190,43 @@ void plan_chunks(const sarathi_kv8_cfg& c, const BatchDesc& b, HostPlan* p) {
       longest = std::max(longest, qbs.back().tiles);
     }
   }
-  // Key ranges: every query block's tiles are cut into near-equal ranges of at
-  // most tau, the tau with the least rounds of blocks x (longest range + the
-  // tiles' worth of a block's set-up and output); the larger on a tie.
+  // Every query block's tiles are cut into near-equal ranges of at most tau;
+  // blocks of one four-wave group, or of two that take the tiles in turn.  The
+  // choice that ends first: the longest range or the rounds of average ones,
+  // with a block's set-up and output, and the combine pass where rows are split.
+  // Two groups finish a block in about half the time without splitting its rows:
+  // 512 rows over 2048 keys of 52 heads (208 blocks) take 58 us, one group 73,
+  // one group with rows split in two 65; a 4096-token prompt of 32 / 8 heads
+  // (1024 blocks), which fills the GPU either way, 196 against 187 of one group.
   int tau = longest;
   double best = 1e300;
-  for (int cand = std::min(PRE_MIN_TILES, longest); cand <= longest; cand += std::max(1, cand / 4)) {
-    long items = 0;
-    int most = 0;
-    for (const QB& q : qbs) {
-      const int ns = ceil_div(q.tiles, cand);
-      items += ns;
-      most = std::max(most, ceil_div(q.tiles, ns));
-    }
-    if (items > (long)qbs.size() + extra_pre(c)) continue;
-    const double cost = (double)ceil_div(items * c.n_kv_heads, PRE_SLOTS) * (most + 4);
-    if (cost <= best) {
-      best = cost;
-      tau = cand;
+  for (int groups = 1; groups <= (c.dtype == SARATHI_BF16 ? 2 : 1); ++groups) {
+    const double fixed = groups == 2 ? PRE_FIXED_TILES_2 : PRE_FIXED_TILES, per_tile = groups == 2 ? PRE_TILE_2 : 1.0;
+    const long slots = PRE_SLOTS / groups;
+    for (int cand = longest;;) {
+      long items = 0, tiles = 0;
+      int most = 0;
+      for (const QB& q : qbs) {
+        const int ns = ceil_div(q.tiles, cand);
+        items += ns;
+        tiles += q.tiles;
+        most = std::max(most, ceil_div(q.tiles, ns));
+      }
+      if (cand == longest || items <= (long)qbs.size() + extra_pre(c)) {
+        const double mean = (double)tiles / std::max(1l, items) / groups;
+        const double rounds = ceil_div(items * c.n_kv_heads, slots) * (mean + fixed);
+        const double cost = std::max(rounds, ceil_div(most, groups) + fixed) * per_tile +
+                            (items > (long)qbs.size() ? PRE_JOIN_TILES : 0);
+        if (cost < best) {
+          best = cost;
+          tau = cand;
+          p->groups = groups;
+        }
+      }
+      cand -= std::max(1, cand / 5);
+      if (cand < PRE_MIN_TILES) break;
     }
   }
-  if (best == 1e300) tau = longest;
   std::vector<int> row0(b.chunks.size());
   int r0 = 0;
   for (size_t ci = 0; ci < b.chunks.size(); ++ci) {
@@ -342,7 +363,7 @@ int plan_upload(const sarathi_kv8* kv, const BatchDesc& b, void* ws, size_t ws_b
   plan->cfg = c; plan->mem = kv->mem; plan->st = kv->st;
   plan->T = T;
   plan->n_chunk_units = h.n_chunk_units; plan->n_units = (int)h.units.size() / 4;
-  plan->n_pre = (int)h.pre.size() / 4; plan->n_dec = (int)h.dec.size() / KV8_DEC_INTS;
+  plan->n_pre = (int)h.pre.size() / 4; plan->groups = h.groups; plan->n_dec = (int)h.dec.size() / KV8_DEC_INTS;
   plan->comb_row0 = h.comb_row0; plan->comb_rows = T - b.B;
   plan->row_slot = rows; plan->row_pos = rows + T; plan->comb = rows + 2 * (size_t)T;
   plan->units = dm + o_units; plan->chunks = dm + o_chunks; plan->pre = dm + o_pre; plan->dec = dm + o_dec;
@@ -386,7 +407,8 @@ int run_attention(const sarathi_kv8_plan* p, int layer, const void* q, size_t ld
   if (p->n_pre > 0) {
     Kv8ChunkArgs a{};
     a.q = q; a.ld_q = ld_q; a.out = out; a.ld_out = ld_out; a.chunks = p->chunks; a.work = p->pre; a.n_work = p->n_pre;
-    a.nh = c.n_heads; a.nkv = c.n_kv_heads; a.part = p->part; a.scale_log2 = scale_log2; a.kv = layer_of(p, layer);
+    a.nh = c.n_heads; a.nkv = c.n_kv_heads; a.groups = p->groups; a.part = p->part; a.scale_log2 = scale_log2;
+    a.kv = layer_of(p, layer);
     e = launch_kv8_chunk(c.dtype, c.format, c.head_dim, a, s);
     if (e != hipSuccess) return hip_fail(e, "chunk attention");
   }
