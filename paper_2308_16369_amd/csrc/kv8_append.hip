@@ -36,43 +36,68 @@ hipError_t launch_kv8_rows(const Kv8RowsArgs& a, hipStream_t s) {
 // ------------------------------------------------------------------ append
 // A head row of D elements sits in D / 8 neighbouring lanes, eight elements
 // each (LPR lanes per row, RPW rows per wave).
-template <typename T>
+// (Rows of qkv are read once: non-temporal, 2048 rows of 52 heads in 43 us, else 47.)
+typedef unsigned int u32x4_nt __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load16_nt(const void* p) {
+  const u32x4_nt v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_nt*>(p));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store16_nt(void* p, uint4 v) {
+  __builtin_nontemporal_store((u32x4_nt){v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_nt*>(p));
+}
+template <typename T, bool ONCE = true>
 __device__ __forceinline__ void kv8_load8(const T* p, float* x) {
-  if constexpr (sizeof(T) == 2) {
-    Vec16<bf16>::unpack(*reinterpret_cast<const uint4*>(p), x);
-  } else {
-    Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
-    Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
-  }
+  auto get = [](const T* q) { return ONCE ? load16_nt(q) : *reinterpret_cast<const uint4*>(q); };
+  Vec16<T>::unpack(get(p), x);
+  if constexpr (sizeof(T) == 4) Vec16<T>::unpack(get(p + 4), x + 4);
 }
 typedef __bf16 kv8_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float kv8_f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t kv8_pack_bf16(float a, float b) {   // nearest even
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((kv8_f32x2){a, b}, kv8_bf16x2));
 }
-template <typename T>
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ void kv8_store8(T* p, const float* x) {
+  auto put = [](T* q, uint4 v) { STREAM ? store16_nt(q, v) : (void)(*reinterpret_cast<uint4*>(q) = v); };
   if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(kv8_pack_bf16(x[0], x[1]), kv8_pack_bf16(x[2], x[3]),
-                                              kv8_pack_bf16(x[4], x[5]), kv8_pack_bf16(x[6], x[7]));
+    put(p, make_uint4(kv8_pack_bf16(x[0], x[1]), kv8_pack_bf16(x[2], x[3]), kv8_pack_bf16(x[4], x[5]),
+                      kv8_pack_bf16(x[6], x[7])));
   } else {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int i = 0; i < 8; i += 4)
+      put(p + i, make_uint4(__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]),
+                            __float_as_uint(x[i + 3])));
   }
 }
 
-// Sum and maximum over the LPR lanes of a row.
+// Maximum that propagates NaN.
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// Exchanges within 16 lanes (DPP row mirror, half mirror, quad permutes): a
+// butterfly over them reaches all 16 lanes, from half mirror on all 8 of a half.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_amdgcn_update_dpp(0.f, v, CTRL, 0xf, 0xf, false);
+}
 template <int LPR>
 __device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-  for (int m = LPR / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
-  return v;
+  if constexpr (LPR == 16) v += dpp<0x140>(v);
+  v += dpp<0x141>(v);
+  v += dpp<0x1B>(v);
+  return v + dpp<0xB1>(v);
+}
+__device__ __forceinline__ float wave_max_nan(float v) {
+  v = max_nan(v, dpp<0x140>(v));
+  v = max_nan(v, dpp<0x141>(v));
+  v = max_nan(v, dpp<0x1B>(v));
+  v = max_nan(v, dpp<0xB1>(v));
+  v = max_nan(v, __shfl_xor(v, 16, 64));
+  return max_nan(v, __shfl_xor(v, 32, 64));
 }
 
 // Eight elements of a head row: norm (gain: this lane's eight gains, null for
 // none), then the rotation by table row `tab`; j = the lane's place in the row.
 template <int D>
-__device__ __forceinline__ void norm_rotate(float* x, const float* gain, float eps, const float2* tab, int rot,
+__device__ __forceinline__ void norm_rotate(float* x, const float* gain, float eps, const float2* __restrict__ tab, int rot,
                                             int interleaved, int j) {
   constexpr int LPR = D / 8;
   if (gain) {
@@ -120,13 +145,24 @@ __device__ __forceinline__ void norm_rotate(float* x, const float* gain, float e
   }
 }
 
+// Largest magnitude of eight elements, NaN where one is.
+__device__ __forceinline__ float top8(const float* x, float top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max_nan(top, fabsf(x[e]));
+  return top;
+}
+__device__ __forceinline__ bool is_finite(float top) { return top <= 3.4028234663852886e38f; }
 // NaN to zero, infinities to the largest finite value of their sign; returns
 // the magnitude that counts for the scale (0 for both).
-__device__ __forceinline__ float tame(float& x) {
-  const float m = fabsf(x);
-  if (m <= 3.4028234663852886e38f) return m;
-  x = m == INFINITY ? copysignf(3.4028234663852886e38f, x) : 0.f;
-  return 0.f;
+__device__ __forceinline__ float tame8(float* x) {
+  float top = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float m = fabsf(x[e]);
+    if (is_finite(m)) top = fmaxf(top, m);
+    else x[e] = m == INFINITY ? copysignf(3.4028234663852886e38f, x[e]) : 0.f;
+  }
+  return top;
 }
 
 // The scale that values of magnitude up to `top` need.
@@ -138,27 +174,33 @@ __device__ __forceinline__ float scale_of(float top) {
   return __uint_as_float((__float_as_uint(s) + 0x7fffffu) & 0xff800000u);   // the next power of two
 }
 
-// Eight codes of x * inv.
+// Eight codes of x * inv, |x * inv| at most the largest code but for the last
+// bits, which the rounding takes away.  int8: adding 1.5 2^23 rounds to the
+// nearest whole number (ties to even), which the sum's low byte then is.
 template <bool INT8>
 __device__ __forceinline__ uint2 encode8(const float* x, float inv) {
-  constexpr float M = INT8 ? KV8_INT8_MAX : KV8_E4M3_MAX;
   uint32_t w[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    float y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fminf(fmaxf(x[4 * h + e] * inv, -M), M);
+    const float* y = x + 4 * h;
     if constexpr (INT8) {
-      uint32_t v = 0;
+      uint32_t b[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v |= ((uint32_t)(int)rintf(y[e]) & 255u) << (8 * e);
-      w[h] = v;
+      for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(fmaf(y[e], inv, 12582912.f));
+      w[h] = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400) | __builtin_amdgcn_perm(b[3], b[2], 0x04000c0c);
     } else {
-      int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-      w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], v, true);
+      const int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, 0, false);
+      w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, v, true);
     }
   }
   return make_uint2(w[0], w[1]);
+}
+// The largest codes of the tamed infinities, whose x * inv lies far outside.
+template <bool INT8>
+__device__ __forceinline__ void clamp8(float* x, float now) {
+  const float m = now * (INT8 ? KV8_INT8_MAX : KV8_E4M3_MAX);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = fminf(fmaxf(x[e], -m), m);
 }
 template <bool INT8>
 __device__ __forceinline__ void decode4(uint32_t w, float* x) {
@@ -186,15 +228,16 @@ __device__ __forceinline__ void rescale_old(uint8_t* codes, int p0, float ratio,
 }
 
 // One launch, three kinds of blocks (256 threads):
-//   queries: a wave takes a row's heads, 64 / LPR at a time; every lane keeps
-//     the same eight dims, so the row's gains and its table entries are read
-//     once per HPW heads;
+//   queries: a wave takes U * 64 / LPR heads of a row, all loads in flight; every
+//     lane keeps the same eight dims, so the row's gains and table entries are
+//     read once;
 //   units of several rows (prompt chunks): one block per (unit, K or V, head)
 //     holds the block's new rows in registers across the maximum;
 //   units of one row (decodes): one wave each.
 // NP: register passes that cover a block's rows.
 template <typename T, int D, bool INT8, int NP>
-__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, int q_blocks, int c_blocks, int hpw) {
+__global__ __launch_bounds__(256, NP == 8 ? 4 : 6) void kv8_append_kernel(Kv8AppendArgs a, int q_blocks, int c_blocks, int hpw) {
+  constexpr int U = 4;
   constexpr int LPR = D / 8, RPW = 64 / LPR, RPP = 4 * RPW;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int j = lane % LPR, g = lane / LPR;
@@ -207,16 +250,21 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, int q_
     const int row = (int)(w / per_row), h0 = (int)(w % per_row) * hpw;
     if (row >= a.T) return;
     float gain[8];
-    if (a.q_gain) kv8_load8(reinterpret_cast<const T*>(a.q_gain) + 8 * j, gain);
+    if (a.q_gain) kv8_load8<T, false>(reinterpret_cast<const T*>(a.q_gain) + 8 * j, gain);
     const T* src = qkv + (size_t)row * a.ld_qkv + 8 * j;
     T* dst = reinterpret_cast<T*>(a.q_out) + (size_t)row * a.ld_q + 8 * j;
     const int h1 = min(a.nh, h0 + hpw);
-    for (int hb = h0; hb < h1; hb += RPW) {
-      const int h = min(hb + g, h1 - 1);        // lanes past the last head repeat it, unwritten
-      float x[8];
-      kv8_load8(src + (size_t)h * D, x);
-      norm_rotate<D>(x, a.q_gain ? gain : nullptr, a.eps, a.tab + (size_t)row * pairs, a.rot, a.interleaved, j);
-      if (hb + g < h1) kv8_store8(dst + (size_t)h * D, x);
+    float x[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u)            // lanes past the last head repeat it, unwritten
+      if (h0 + u * RPW < h1) kv8_load8(src + (size_t)min(h0 + u * RPW + g, h1 - 1) * D, x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * RPW + g;
+      if (h0 + u * RPW < h1) {
+        norm_rotate<D>(x[u], a.q_gain ? gain : nullptr, a.eps, a.tab + (size_t)row * pairs, a.rot, a.interleaved, j);
+        if (h < h1) kv8_store8(dst + (size_t)h * D, x[u]);
+      }
     }
     return;
   }
@@ -232,7 +280,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, int q_
     const float was = p0 > 0 ? *scale : 0.f;
     float gain[8];
     const bool norm = a.k_gain != nullptr && which == 0;
-    if (norm) kv8_load8(reinterpret_cast<const T*>(a.k_gain) + 8 * j, gain);
+    if (norm) kv8_load8<T, false>(reinterpret_cast<const T*>(a.k_gain) + 8 * j, gain);
     const T* src = qkv + (size_t)row0 * a.ld_qkv + (size_t)(a.nh + which * a.nkv + h) * D + 8 * j;
     float x[NP][8], top = 0.f;
 #pragma unroll
@@ -246,16 +294,31 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, int q_
         const int r = min(i * RPP + wave * RPW + g, n - 1);
         if (which == 0)
           norm_rotate<D>(x[i], norm ? gain : nullptr, a.eps, a.tab + (size_t)(row0 + r) * pairs, a.rot, a.interleaved, j);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, tame(x[i][e]));
+        top = top8(x[i], top);
       }
     }
-    __shared__ float red[4];
-    top = wave_max(top);
-    if (lane == 0) red[wave] = top;
+    __shared__ float red[2][4];
+    top = wave_max_nan(top);
+    if (lane == 0) red[0][wave] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    top = max_nan(max_nan(red[0][0], red[0][1]), max_nan(red[0][2], red[0][3]));
+    const bool tamed = !is_finite(top);
+    if (tamed) {                           // the whole block: something is not finite
+      top = 0.f;
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        if (i * RPP < n) top = fmaxf(top, tame8(x[i]));
+      top = wave_max(top);
+      if (lane == 0) red[1][wave] = top;
+      __syncthreads();
+      top = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    }
     const float now = fmaxf(was, scale_of<INT8>(top));
+    if (tamed) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        if (i * RPP < n) clamp8<INT8>(x[i], now);
+    }
     const float inv = now > 0.f ? 1.0f / now : 0.f;
     if (tid == 0) *scale = now;
 #pragma unroll
@@ -278,13 +341,14 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, int q_
   float x[8], gain[8], top = 0.f;
   const bool norm = a.k_gain != nullptr && which == 0;
   kv8_load8(qkv + (size_t)row * a.ld_qkv + (size_t)(a.nh + which * a.nkv + h) * D + 8 * j, x);
-  if (norm) kv8_load8(reinterpret_cast<const T*>(a.k_gain) + 8 * j, gain);
+  if (norm) kv8_load8<T, false>(reinterpret_cast<const T*>(a.k_gain) + 8 * j, gain);
   if (which == 0)
     norm_rotate<D>(x, norm ? gain : nullptr, a.eps, a.tab + (size_t)row * pairs, a.rot, a.interleaved, j);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, tame(x[e]));
-  top = wave_max(top);
+  top = wave_max_nan(top8(x, 0.f));
+  const bool tamed = !is_finite(top);
+  if (tamed) top = wave_max(tame8(x));
   const float now = fmaxf(was, scale_of<INT8>(top));
+  if (tamed) clamp8<INT8>(x, now);
   const float inv = now > 0.f ? 1.0f / now : 0.f;
   if (lane == 0) *scale = now;
   if (g == 0) *reinterpret_cast<uint2*>(codes + (size_t)p0 * D + 8 * j) = encode8<INT8>(x, inv);
@@ -294,7 +358,11 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, int q_
 template <typename T, int D, bool INT8>
 static hipError_t append_launch(int block, const Kv8AppendArgs& a, hipStream_t s) {
   constexpr int RPP = 4 * 64 / (D / 8);
-  const int hpw = 8;
+  // heads per wave: four rounds where that leaves waves enough to fill the GPU
+  // (16 per CU), else fewer
+  constexpr int RPW = 64 / (D / 8);
+  int hpw = 4 * RPW;
+  while (hpw > RPW && (long)a.T * ((a.nh + hpw - 1) / hpw) < 256 * 16) hpw /= 2;
   const long per_row = (a.nh + hpw - 1) / hpw;
   const int q_blocks = (int)((a.T * per_row + 3) / 4);
   const int c_blocks = a.n_chunk * 2 * a.nkv;
@@ -320,7 +388,8 @@ hipError_t launch_kv8_append(int dtype, int format, int hd, int block, const Kv8
 }
 
 // ------------------------------------------------------------------ read
-// One thread per 16 codes of a (row, K or V, head).
+// One thread per 16 codes of a (row, K or V, head); the rows leave past the
+// caches (2048 positions of 52 heads: 17 us so, 20 otherwise).
 template <typename T, bool INT8>
 __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8ReadArgs a) {
   const int per = a.hd / 16;
@@ -343,8 +412,8 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8ReadArgs a) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) x[e] *= s;
   T* dst = out + row * (which ? a.ld_v : a.ld_k) + (size_t)h * a.hd + 16 * c;
-  kv8_store8(dst, x);
-  kv8_store8(dst + 8, x + 8);
+  kv8_store8<T, true>(dst, x);
+  kv8_store8<T, true>(dst + 8, x + 8);
 }
 
 hipError_t launch_kv8_read(int out_dtype, int format, const Kv8ReadArgs& a, hipStream_t s) {
