@@ -171,6 +171,39 @@ int sarathi_kv8_attention(const sarathi_kv8_plan* plan, int layer, const void* q
 int sarathi_kv8_read(const sarathi_kv8_plan* plan, int layer, int out_dtype, void* k_out, size_t ld_k, void* v_out,
                      size_t ld_v, void* hip_stream);
 
+/* ------------------------------------------------------------------ decoder layer */
+/*
+ * One decoder layer, and a stack of them, over a mixed batch with the 8-bit
+ * cache: sarathi_mixed_layer_forward / sarathi_mixed_model_step (sarathi.h)
+ * with its rotary embedding, append and attention replaced by the operators
+ * above (the batch is planned once per call):
+ *   a = norm_1(x); [q|k|v] = a W_qkv^T; append; o = attention;
+ *   h = x + o W_o^T; m = act(norm_2(h) W_up^T); y = h + m W_down^T.
+ * w_qkv is [(n_heads + 2 n_kv_heads) * head_dim, hidden]; q_gain, k_gain
+ * [head_dim] are used with qk_norm.  cfg must agree with the cache's cfg in
+ * n_heads, head_dim, n_layers, dtype, and in rope (rope_dim > 0) and rope_base.
+ * Arguments, aliasing rules and errors otherwise as sarathi_mixed_layer_forward;
+ * workspace: sarathi_kv8_workspace_bytes.  The intermediates that
+ * sarathi_kv8_workspace_layout places hold the (last) layer's values after a
+ * call (qkv: q normalised and rotated, k and v as projected).
+ */
+typedef struct {
+  sarathi_layer_weights base;
+  const void* q_gain;
+  const void* k_gain;
+} sarathi_kv8_layer_weights;
+
+size_t sarathi_kv8_workspace_bytes(const sarathi_model_cfg* cfg, const sarathi_kv8_cfg* kv_cfg, int max_tokens,
+                                   int max_chunks, int max_seq_len);
+int sarathi_kv8_workspace_layout(const sarathi_model_cfg* cfg, const sarathi_kv8_cfg* kv_cfg, int n_tokens,
+                                 int n_chunks, int max_seq_len, sarathi_ws_layout* out);
+int sarathi_kv8_layer_forward(const sarathi_model_cfg* cfg, const sarathi_kv8_layer_weights* w, const sarathi_kv8* kv,
+                              int layer, const sarathi_mixed_batch* batch, const void* x_in, void* x_out, void* ws,
+                              size_t ws_bytes, void* hip_stream);
+int sarathi_kv8_model_step(const sarathi_model_cfg* cfg, const sarathi_kv8_layer_weights* w, const sarathi_kv8* kv,
+                           const sarathi_mixed_batch* batch, const void* x_in, void* x_out, void* ws, size_t ws_bytes,
+                           void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -303,7 +303,7 @@ int host_plan(const sarathi_kv8_cfg& c, const BatchDesc& b, HostPlan* p) {
     if (p->spans[i + 5] > 0) p->comb_row0 = std::min(p->comb_row0, p->spans[i + 2]);
   const long T = b.rows(), units = (long)p->units.size() / 4;
   const long grids[] = {(long)p->pre.size() / 4 * c.n_kv_heads, (long)p->dec.size() / KV8_DEC_INTS * c.n_kv_heads * head_blocks(c),
-                        T * ((c.n_heads + 7) / 8) + units * 2 * c.n_kv_heads, T * 2 * c.n_kv_heads * (c.head_dim / 16) / 256 + 1};
+                        T * ((c.n_heads + 3) / 4) + units * 2 * c.n_kv_heads, T * 2 * c.n_kv_heads * (c.head_dim / 16) / 256 + 1};
   for (long g : grids)
     if (g > MAX_GRID) return fail(SARATHI_EUNSUPPORTED, "batch of %ld rows x %d heads needs more than %ld blocks", T, c.n_heads, MAX_GRID);
   return SARATHI_OK;
@@ -425,6 +425,134 @@ int run_attention(const sarathi_kv8_plan* p, int layer, const void* q, size_t ld
   ca.out = out; ca.ld_out = (int)ld_out;
   e = launch_attn_combine(c.dtype, ca, s);
   return e == hipSuccess ? SARATHI_OK : hip_fail(e, "attention combine");
+}
+
+// ---- decoder layer
+struct LayerLayout {
+  size_t a, qkv, o, hres, m, parts, ping0, ping1, plan, total;
+};
+LayerLayout layer_layout(const sarathi_model_cfg& c, const sarathi_kv8_cfg& k, int T, int n_chunks) {
+  LayerLayout L{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off = align256(off + bytes); return at; };
+  const size_t es = esize(c.dtype), H = c.hidden, hd = k.head_dim;
+  L.a = take(T * H * es);
+  L.qkv = take(T * (k.n_heads + 2 * (size_t)k.n_kv_heads) * hd * es);
+  L.o = take(T * k.n_heads * hd * es);
+  L.hres = take(T * H * 4);
+  L.m = take(T * (size_t)c.ffn * es);
+  L.parts = take((size_t)MAX_SPLIT * std::min(T, PARTS_ROWS) * H * 4);
+  L.ping0 = take(T * H * es);
+  L.ping1 = take(T * H * es);
+  L.plan = take(plan_layout(k, T, n_chunks).total);
+  L.total = off;
+  return L;
+}
+
+// cfg on its own and against the cache's.
+int check_layer_cfg(const sarathi_model_cfg* c, const sarathi_kv8_cfg* k) {
+  int rc = check_cfg(c);
+  if (!rc) rc = check_kv8_cfg(k);
+  if (rc) return rc;
+  if (c->n_heads != k->n_heads || c->head_dim != k->head_dim || c->n_layers != k->n_layers || c->dtype != k->dtype ||
+      c->rope != (k->rope_dim > 0) || (c->rope && c->rope_base != k->rope_base))
+    return fail(SARATHI_EINVAL, "cfg differs from the cfg of the 8-bit KV cache");
+  return SARATHI_OK;
+}
+
+// One layer of a planned batch.  norm1_ready, next, next_norm1_done: as in the
+// 16-bit layer (norm_1 folded into the previous layer's last reduction).
+int layer_body(const sarathi_model_cfg* c, const LayerLayout& L, const sarathi_kv8_plan* plan,
+               const sarathi_kv8_layer_weights* w, int layer, const void* x_in, void* x_out, char* ws, hipStream_t s,
+               bool norm1_ready, const sarathi_kv8_layer_weights* next, bool* next_norm1_done) {
+  const int T = plan->T, H = c->hidden, F = c->ffn, dt = c->dtype;
+  const int QD = c->n_heads * c->head_dim, N = QD + 2 * plan->cfg.n_kv_heads * c->head_dim;
+  const bool ln = c->norm == SARATHI_NORM_LAYER;
+  float* hres = reinterpret_cast<float*>(ws + L.hres);
+  float* parts = reinterpret_cast<float*>(ws + L.parts);
+  const size_t parts_cap = (size_t)MAX_SPLIT * std::min(T, PARTS_ROWS) * H;
+  hipError_t e;
+  if (!norm1_ready) {
+    e = launch_norm(dt, false, ln, x_in, w->base.norm1_g, w->base.norm1_b, ws + L.a, T, H, c->eps, s);
+    if (e != hipSuccess) return hip_fail(e, "norm_1");
+  }
+  LinearArgs q{};
+  q.kind = LIN_PLAIN; q.M = T; q.N = N; q.K = H; q.x = ws + L.a; q.w = w->base.w_qkv; q.out = ws + L.qkv;
+  e = launch_linear(dt, q, s);
+  if (e != hipSuccess) return hip_fail(e, "preproj");
+  int rc = run_append(plan, layer, ws + L.qkv, N, w->q_gain, w->k_gain, ws + L.qkv, N, s);
+  if (!rc) rc = run_attention(plan, layer, ws + L.qkv, N, ws + L.o, QD, s);
+  if (rc) return rc;
+  NormArgs n2{w->base.norm2_g, w->base.norm2_b, ws + L.a, c->eps, ln};
+  bool norm2_done = false;
+  LinearArgs po{};
+  po.kind = LIN_RESID; po.M = T; po.N = H; po.K = QD; po.x = ws + L.o; po.w = w->base.w_o; po.resid = x_in; po.out = hres;
+  po.parts = parts; po.parts_cap = parts_cap; po.norm = &n2; po.norm_done = &norm2_done;
+  e = launch_linear(dt, po, s);
+  if (e != hipSuccess) return hip_fail(e, "postproj");
+  if (!norm2_done) {
+    e = launch_norm(dt, true, ln, hres, w->base.norm2_g, w->base.norm2_b, ws + L.a, T, H, c->eps, s);
+    if (e != hipSuccess) return hip_fail(e, "norm_2");
+  }
+  LinearArgs up{};
+  up.kind = c->act == SARATHI_ACT_SWIGLU ? LIN_SWIGLU : LIN_GELU;
+  up.M = T; up.N = F; up.K = H; up.x = ws + L.a; up.w = w->base.w_up; up.out = ws + L.m;
+  e = launch_linear(dt, up, s);
+  if (e != hipSuccess) return hip_fail(e, "ffn_ln1");
+  LinearArgs dn{};
+  dn.kind = LIN_RESID_F32IN; dn.M = T; dn.N = H; dn.K = F; dn.x = ws + L.m; dn.w = w->base.w_down; dn.resid = hres;
+  dn.out = x_out; dn.parts = parts; dn.parts_cap = parts_cap;
+  NormArgs n1{};
+  if (next) {
+    n1 = NormArgs{next->base.norm1_g, next->base.norm1_b, ws + L.a, c->eps, ln};
+    dn.norm = &n1; dn.norm_done = next_norm1_done;
+  }
+  e = launch_linear(dt, dn, s);
+  return e == hipSuccess ? SARATHI_OK : hip_fail(e, "ffn_ln2");
+}
+
+// Layers first .. first + n - 1 over one batch, each with its entry of w.
+int run_layers(const sarathi_model_cfg* cfg, const sarathi_kv8_layer_weights* w, const sarathi_kv8* kv, int first, int n,
+               const sarathi_mixed_batch* batch, const void* x_in, void* x_out, void* ws, size_t ws_bytes, hipStream_t s) {
+  int rc = check_layer_cfg(cfg, &kv->cfg);
+  if (rc) return rc;
+  if (first < 0 || first + n > cfg->n_layers) return fail(SARATHI_EINVAL, "layer %d outside [0, %d)", first, cfg->n_layers);
+  BatchDesc b;
+  rc = from_mixed(batch, &b);
+  if (!rc) rc = check_batch(b, kv->n_slots, kv->max_seq_len);
+  if (rc) return rc;
+  if (!w) return fail(SARATHI_EINVAL, "weights are NULL");
+  for (int i = 0; i < n; ++i) {
+    rc = check_weights(cfg, &w[i].base, first + i);
+    if (rc) return rc;
+    if (kv->cfg.qk_norm && (!w[i].q_gain || !w[i].k_gain || !aligned16(w[i].q_gain) || !aligned16(w[i].k_gain)))
+      return fail(SARATHI_EINVAL, "layer %d: qk_norm needs 16-byte aligned q_gain and k_gain", first + i);
+  }
+  if (!x_in || !x_out || !ws) return fail(SARATHI_EINVAL, "x_in, x_out or the workspace is NULL");
+  if (!aligned16(x_in) || !aligned16(x_out) || !aligned16(ws))
+    return fail(SARATHI_EINVAL, "x_in, x_out and ws must be 16-byte aligned");
+  const int T = b.rows();
+  const LayerLayout L = layer_layout(*cfg, kv->cfg, T, (int)b.chunks.size());
+  if (ws_bytes < L.total) return fail(SARATHI_ENOSPC, "workspace of %zu bytes < %zu needed", ws_bytes, L.total);
+  const size_t xb = (size_t)T * cfg->hidden * esize(cfg->dtype);
+  const Span xi{static_cast<const char*>(x_in), xb}, xo{static_cast<const char*>(x_out), xb}, wsp{static_cast<const char*>(ws), L.total};
+  if (overlap(xi, xo) || overlap(xi, wsp) || overlap(xo, wsp))
+    return fail(SARATHI_EINVAL, "x_in, x_out and the workspace must not overlap");
+  char* base = static_cast<char*>(ws);
+  sarathi_kv8_plan plan{};
+  rc = plan_upload(kv, b, base + L.plan, L.total - L.plan, s, &plan);
+  if (rc) return rc;
+  char* ping[2] = {base + L.ping0, base + L.ping1};
+  bool ready = false;
+  for (int i = 0; i < n; ++i) {
+    const void* in = i == 0 ? x_in : ping[i & 1];
+    void* out = i == n - 1 ? x_out : ping[(i + 1) & 1];
+    bool next_ready = false;
+    rc = layer_body(cfg, L, &plan, w + i, first + i, in, out, base, s, ready, i + 1 < n ? w + i + 1 : nullptr, &next_ready);
+    if (rc) return rc;
+    ready = next_ready;
+  }
+  return SARATHI_OK;
 }
 
 // No C++ exception leaves a C entry (the host lists are the only allocations).
@@ -552,6 +680,42 @@ int sarathi_kv8_read(const sarathi_kv8_plan* plan, int layer, int out_dtype, voi
   a.T = plan->T; a.nkv = c.n_kv_heads; a.hd = c.head_dim; a.kv = layer_of(plan, layer);
   const hipError_t e = launch_kv8_read(out_dtype, c.format, a, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? SARATHI_OK : hip_fail(e, "read");
+}
+
+size_t sarathi_kv8_workspace_bytes(const sarathi_model_cfg* cfg, const sarathi_kv8_cfg* kv_cfg, int max_tokens,
+                                   int max_chunks, int max_seq_len) {
+  if (check_layer_cfg(cfg, kv_cfg) != SARATHI_OK || max_tokens < 1 || max_chunks < 0 || max_seq_len < 1) return 0;
+  return layer_layout(*cfg, *kv_cfg, max_tokens, max_chunks).total;
+}
+
+int sarathi_kv8_workspace_layout(const sarathi_model_cfg* cfg, const sarathi_kv8_cfg* kv_cfg, int n_tokens, int n_chunks,
+                                 int max_seq_len, sarathi_ws_layout* out) {
+  const int rc = check_layer_cfg(cfg, kv_cfg);
+  if (rc) return rc;
+  if (!out) return fail(SARATHI_EINVAL, "out is NULL");
+  if (n_tokens < 1 || n_chunks < 0 || max_seq_len < 1) return fail(SARATHI_EINVAL, "bad sizes");
+  const LayerLayout L = layer_layout(*cfg, *kv_cfg, n_tokens, n_chunks);
+  out->a = L.a; out->qkv = L.qkv; out->o = L.o; out->hres = L.hres; out->m = L.m;
+  out->ping[0] = L.ping0; out->ping[1] = L.ping1; out->total = L.total;
+  return SARATHI_OK;
+}
+
+int sarathi_kv8_layer_forward(const sarathi_model_cfg* cfg, const sarathi_kv8_layer_weights* w, const sarathi_kv8* kv,
+                              int layer, const sarathi_mixed_batch* batch, const void* x_in, void* x_out, void* ws,
+                              size_t ws_bytes, void* hip_stream) {
+  if (!kv) return fail(SARATHI_EINVAL, "kv is NULL");
+  return guarded([&] {
+    return run_layers(cfg, w, kv, layer, 1, batch, x_in, x_out, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int sarathi_kv8_model_step(const sarathi_model_cfg* cfg, const sarathi_kv8_layer_weights* w, const sarathi_kv8* kv,
+                           const sarathi_mixed_batch* batch, const void* x_in, void* x_out, void* ws, size_t ws_bytes,
+                           void* hip_stream) {
+  if (!kv) return fail(SARATHI_EINVAL, "kv is NULL");
+  return guarded([&] {
+    return run_layers(cfg, w, kv, 0, kv->cfg.n_layers, batch, x_in, x_out, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+  });
 }
 
 }  // extern "C"

@@ -54,8 +54,6 @@ constexpr int PRE_SPLIT = 256;    // smallest key split of a chunk-attention wor
 constexpr int QBLOCK = PREFILL_QBLOCK;   // chunk rows per chunk-attention work item (the larger size)
 constexpr double SMALL_BLOCK_TILE = 0.82;   // bf16: a 128-row block's time per key tile, a 256-row one's being 1
 constexpr double F32_TILE_US_64 = 2.46, F32_TILE_US_128 = 4.43;   // fp32 chunk block per 64-key tile, by head_dim
-constexpr int PARTS_ROWS = 512;   // split-K partials are sized for batches up to this many rows (larger
-                                  // batches fill the GPU without splitting; with less room fewer splits run)
 
 size_t esize(const sarathi_model_cfg* c) { return c->dtype == SARATHI_BF16 ? 2 : 4; }
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }

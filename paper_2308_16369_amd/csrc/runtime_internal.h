@@ -9,6 +9,9 @@
 
 namespace sarathi {
 
+constexpr int PARTS_ROWS = 512;   // split-K partials are sized for batches up to this many rows (larger
+                                  // batches fill the GPU without splitting; with less room fewer splits run)
+
 // A batch of any number of prompt chunks plus decodes (the hybrid batch of
 // the paper has at most one chunk).
 struct ChunkDesc {

@@ -87,6 +87,10 @@ class sarathi_kv8_cfg(ct.Structure):
          ("rope_low", ct.c_float), ("rope_high", ct.c_float), ("rope_orig_len", ct.c_int), ("rope_mscale", ct.c_float)]
 
 
+class sarathi_kv8_layer_weights(ct.Structure):
+    _fields_ = [("base", sarathi_layer_weights), ("q_gain", ct.c_void_p), ("k_gain", ct.c_void_p)]
+
+
 class sarathi_kv8_layout(ct.Structure):
     _fields_ = [(n, ct.c_size_t) for n in ("layer", "slot", "kv", "head", "pos", "scale_layer", "scale_slot", "scale_kv",
                                            "scale_head", "scale_offset")]
@@ -172,6 +176,16 @@ EXPORTS = {
                                          ct.c_void_p]),
     "sarathi_kv8_read": (ct.c_int, [ct.c_void_p, ct.c_int, ct.c_int, ct.c_void_p, ct.c_size_t, ct.c_void_p,
                                     ct.c_size_t, ct.c_void_p]),
+    "sarathi_kv8_workspace_bytes": (ct.c_size_t, [ct.POINTER(sarathi_model_cfg), ct.POINTER(sarathi_kv8_cfg), ct.c_int,
+                                                  ct.c_int, ct.c_int]),
+    "sarathi_kv8_workspace_layout": (ct.c_int, [ct.POINTER(sarathi_model_cfg), ct.POINTER(sarathi_kv8_cfg), ct.c_int,
+                                                ct.c_int, ct.c_int, ct.POINTER(sarathi_ws_layout)]),
+    "sarathi_kv8_layer_forward": (ct.c_int, [ct.POINTER(sarathi_model_cfg), ct.POINTER(sarathi_kv8_layer_weights),
+                                             ct.c_void_p, ct.c_int, ct.POINTER(sarathi_mixed_batch), ct.c_void_p,
+                                             ct.c_void_p, ct.c_void_p, ct.c_size_t, ct.c_void_p]),
+    "sarathi_kv8_model_step": (ct.c_int, [ct.POINTER(sarathi_model_cfg), ct.POINTER(sarathi_kv8_layer_weights),
+                                          ct.c_void_p, ct.POINTER(sarathi_mixed_batch), ct.c_void_p, ct.c_void_p,
+                                          ct.c_void_p, ct.c_size_t, ct.c_void_p]),
     "sarathi_sched_create": (ct.c_int, [ct.POINTER(sarathi_sched_cfg), ct.POINTER(ct.c_void_p)]),
     "sarathi_sched_destroy": (None, [ct.c_void_p]),
     "sarathi_sched_submit": (ct.c_int, [ct.c_void_p, ct.c_int, ct.c_int, ct.POINTER(ct.c_int)]),
@@ -502,6 +516,37 @@ def sarathi_kv8_attention(plan: KV8Plan, layer: int, q: int, ld_q: int, out: int
 def sarathi_kv8_read(plan: KV8Plan, layer: int, out_dtype: int, k_out: int, ld_k: int, v_out: int, ld_v: int,
                      stream: int = 0, check: bool = True) -> int:
     rc = lib().sarathi_kv8_read(plan.handle, layer, out_dtype, k_out or None, ld_k, v_out or None, ld_v, stream)
+    return _check(rc) if check else rc
+
+
+def make_kv8_weights(ptrs: dict) -> sarathi_kv8_layer_weights:
+    """make_weights plus q_gain and k_gain (qk_norm)."""
+    gain = lambda k: ct.c_void_p(int(ptrs[k])) if ptrs.get(k) else None
+    return sarathi_kv8_layer_weights(make_weights(ptrs), gain("q_gain"), gain("k_gain"))
+
+
+def sarathi_kv8_workspace_bytes(cfg, kv_cfg, max_tokens: int, max_chunks: int, max_seq_len: int) -> int:
+    return lib().sarathi_kv8_workspace_bytes(ct.byref(cfg), ct.byref(kv_cfg), max_tokens, max_chunks, max_seq_len)
+
+
+def sarathi_kv8_workspace_layout(cfg, kv_cfg, n_tokens: int, n_chunks: int, max_seq_len: int) -> sarathi_ws_layout:
+    out = sarathi_ws_layout()
+    _check(lib().sarathi_kv8_workspace_layout(ct.byref(cfg), ct.byref(kv_cfg), n_tokens, n_chunks, max_seq_len,
+                                              ct.byref(out)))
+    return out
+
+
+def sarathi_kv8_layer_forward(cfg, weights: sarathi_kv8_layer_weights, kv: KV8, layer: int, batch, x_in: int, x_out: int,
+                              ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_kv8_layer_forward(ct.byref(cfg), ct.byref(weights), kv.handle, layer, ct.byref(batch), x_in, x_out,
+                                         ws, ws_bytes, stream)
+    return _check(rc) if check else rc
+
+
+def sarathi_kv8_model_step(cfg, weights: Sequence[sarathi_kv8_layer_weights], kv: KV8, batch, x_in: int, x_out: int,
+                           ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
+    arr = (sarathi_kv8_layer_weights * len(weights))(*weights)
+    rc = lib().sarathi_kv8_model_step(ct.byref(cfg), arr, kv.handle, ct.byref(batch), x_in, x_out, ws, ws_bytes, stream)
     return _check(rc) if check else rc
 
 

@@ -34,14 +34,24 @@ POLICY_NAMES = {S.POLICY_DECODE_MAXIMAL: "decode-maximal", S.POLICY_PREFILL_DECO
                 S.POLICY_MIXED: "mixed"}
 
 
+def kv8_config(shape, n_layers: int, fmt: str, block: int):
+    """The 8-bit cache of a layer shape (every head has its own keys and values, rotated as in the 16-bit cache)."""
+    return S.make_kv8_cfg(shape.n_heads, shape.n_heads, shape.head_dim, n_layers=n_layers,
+                          dtype=S.BF16 if shape.dtype == "bf16" else S.F32, block=block,
+                          format={"int8": S.KV8_INT8, "e4m3": S.KV8_E4M3}[fmt],
+                          rope_dim=shape.head_dim if shape.rope else 0, rope_base=shape.rope_base)
+
+
 class ServeModel:
     """L layers of weights, a KV cache of n_slots x max_seq_len positions and
     a workspace for max_tokens rows, all on the current device.  Weights come
     from host arrays (``weights``: list of per-layer dicts) or are drawn on
-    the device (0.02 * N(0,1); gains 1 + 0.02 * N(0,1))."""
+    the device (0.02 * N(0,1); gains 1 + 0.02 * N(0,1)).  kv8 ("int8" or
+    "e4m3"): the KV cache in 8 bits, one scale per kv8_block positions."""
 
     def __init__(self, shape, n_layers: int, n_slots: int, max_seq_len: int, max_tokens: int,
-                 weights: Optional[List[dict]] = None, seed: int = 0, max_chunks: int = 1):
+                 weights: Optional[List[dict]] = None, seed: int = 0, max_chunks: int = 1,
+                 kv8: Optional[str] = None, kv8_block: int = 64):
         import numpy as np
         import torch
 
@@ -70,13 +80,21 @@ class ServeModel:
                     mean, std = (1.0, 0.02) if k.endswith("_g") else (0.0, 0.02)
                     lw[k] = torch.empty(dim, dtype=self.tdt, device="cuda").normal_(mean, std, generator=g)
             self.w.append(lw)
-        self.wabi = (S.sarathi_layer_weights * n_layers)(
-            *[S.make_weights({k: t.data_ptr() for k, t in lw.items()}) for lw in self.w])
-        self.kv_t = torch.zeros((n_layers, n_slots, 2, nh, max_seq_len, d), dtype=self.tdt, device="cuda")
-        self.kv = S.sarathi_kv_alloc(self.cfg, n_slots, max_seq_len, self.kv_t.data_ptr(),
-                                     self.kv_t.numel() * self.kv_t.element_size())
+        ptrs = [{k: t.data_ptr() for k, t in lw.items()} for lw in self.w]
+        self.kv8_cfg = kv8_config(shape, n_layers, kv8, kv8_block) if kv8 else None
+        if kv8:
+            self.wabi = (S.sarathi_kv8_layer_weights * n_layers)(*[S.make_kv8_weights(p) for p in ptrs])
+            size = S.sarathi_kv8_bytes(self.kv8_cfg, n_slots, max_seq_len)
+            self.kv_t = torch.zeros(size, dtype=torch.uint8, device="cuda")
+            self.kv = S.sarathi_kv8_alloc(self.kv8_cfg, n_slots, max_seq_len, self.kv_t.data_ptr(), size)
+            self.ws_bytes = S.sarathi_kv8_workspace_bytes(self.cfg, self.kv8_cfg, max_tokens, max_chunks, max_seq_len)
+        else:
+            self.wabi = (S.sarathi_layer_weights * n_layers)(*[S.make_weights(p) for p in ptrs])
+            self.kv_t = torch.zeros((n_layers, n_slots, 2, nh, max_seq_len, d), dtype=self.tdt, device="cuda")
+            self.kv = S.sarathi_kv_alloc(self.cfg, n_slots, max_seq_len, self.kv_t.data_ptr(),
+                                         self.kv_t.numel() * self.kv_t.element_size())
+            self.ws_bytes = S.sarathi_mixed_workspace_bytes(self.cfg, max_tokens, max_chunks, max_seq_len)
         self.n_slots, self.max_seq_len, self.max_tokens, self.max_chunks = n_slots, max_seq_len, max_tokens, max_chunks
-        self.ws_bytes = S.sarathi_mixed_workspace_bytes(self.cfg, max_tokens, max_chunks, max_seq_len)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")
         self.x = torch.empty((max_tokens, H), dtype=self.tdt, device="cuda").normal_(0.0, 1.0, generator=g)
         self.y = torch.empty_like(self.x)
@@ -86,10 +104,10 @@ class ServeModel:
         """One model iteration over a sarathi_mixed_batch (any number of chunks)."""
         lib = S.lib()
         import ctypes as ct
-        rc = lib.sarathi_mixed_model_step(ct.byref(self.cfg), self.wabi, self.kv.handle, ct.byref(bb),
-                                          ct.c_void_p(x.data_ptr()), ct.c_void_p(y.data_ptr()),
-                                          ct.c_void_p(self.ws.data_ptr()), self.ws_bytes,
-                                          ct.c_void_p(self.stream.cuda_stream))
+        step = lib.sarathi_kv8_model_step if self.kv8_cfg else lib.sarathi_mixed_model_step
+        rc = step(ct.byref(self.cfg), self.wabi, self.kv.handle, ct.byref(bb), ct.c_void_p(x.data_ptr()),
+                  ct.c_void_p(y.data_ptr()), ct.c_void_p(self.ws.data_ptr()), self.ws_bytes,
+                  ct.c_void_p(self.stream.cuda_stream))
         S._check(rc)
 
 
@@ -208,16 +226,19 @@ def to_markdown(res: dict) -> str:
     return "\n".join(L) + "\n"
 
 
-def equation_batch(shape, n_layers: int, seq_len: int, mem_gpu: int, headroom: int = 0) -> dict:
+def equation_batch(shape, n_layers: int, seq_len: int, mem_gpu: int, headroom: int = 0, kv8_block: int = 0) -> dict:
     """The decode batch of Sec. 4.3.1, B = floor((M_G - M_S) / (L * m_kv)):
     M_G the device memory (less ``headroom`` for activations and the
     workspace), M_S the bytes of the model's weights, L the sequence length
-    and m_kv the K and V bytes of one token over all layers."""
+    and m_kv the K and V bytes of one token over all layers (kv8_block: of the
+    8-bit cache with scales of that many positions)."""
     es = 2 if shape.dtype == "bf16" else 4
     H, nh, d, F = shape.hidden, shape.n_heads, shape.head_dim, shape.ffn
     per_layer = (3 * nh * d * H + H * nh * d + shape.up_rows * H + H * F + 2 * H) * es
     m_s = n_layers * per_layer
     m_kv = n_layers * 2 * nh * d * es
+    if kv8_block:
+        m_kv = -(-n_layers * 2 * nh * (d * kv8_block + 4) // kv8_block)
     b = accounting.max_decode_batch(mem_gpu - headroom, m_s, seq_len, m_kv)
     return {"B": b, "mem_gpu": mem_gpu, "headroom": headroom, "mem_params": m_s, "kv_bytes_per_token": m_kv,
             "seq_len": seq_len}
@@ -237,6 +258,8 @@ def main(argv: Optional[Sequence[str]] = None) -> int:
     ap.add_argument("--requests", type=int, default=0, help="requests per run (default 2 x batch)")
     ap.add_argument("--mixed", action="store_true", help="also run Orca-style mixed batching")
     ap.add_argument("--mixed-chunks", type=int, default=4, help="prompts per mixed iteration")
+    ap.add_argument("--kv8", choices=["int8", "e4m3"], default=None, help="KV cache in 8 bits")
+    ap.add_argument("--kv8-block", type=int, default=64, help="positions per scale of the 8-bit cache")
     ap.add_argument("--json", default=None)
     ap.add_argument("--md", default=None)
     args = ap.parse_args(argv)
@@ -250,7 +273,8 @@ def main(argv: Optional[Sequence[str]] = None) -> int:
     eq = None
     if args.batch <= 0:
         mem = int(args.mem_gb * 1e9) if args.mem_gb > 0 else torch.cuda.get_device_properties(0).total_memory
-        eq = equation_batch(shape, args.layers, max(args.seq), mem, headroom=8 << 30)
+        eq = equation_batch(shape, args.layers, max(args.seq), mem, headroom=8 << 30,
+                            kv8_block=args.kv8_block if args.kv8 else 0)
         args.batch = eq["B"] if args.max_batch <= 0 else min(eq["B"], args.max_batch)
         print(f"# B = {args.batch} from Sec. 4.3.1: floor(({eq['mem_gpu'] / 1e9:.1f} GB - {eq['headroom'] / 1e9:.1f} GB "
               f"headroom - {eq['mem_params'] / 1e9:.2f} GB weights) / ({eq['seq_len']} x "
@@ -266,10 +290,11 @@ def main(argv: Optional[Sequence[str]] = None) -> int:
         max_tokens = max(max_tokens, args.mixed_chunks * max(args.seq) + args.batch)
     t0 = time.time()
     log = lambda s: print(f"# {s} ({time.time() - t0:.1f}s)", file=sys.stderr, flush=True)
-    m = ServeModel(shape, args.layers, args.batch, max_seq, max_tokens, max_chunks=max_chunks)
+    m = ServeModel(shape, args.layers, args.batch, max_seq, max_tokens, max_chunks=max_chunks, kv8=args.kv8,
+                   kv8_block=args.kv8_block)
     log(f"{args.layers}-layer model on the device")
     run_schedule(m, S.POLICY_DECODE_MAXIMAL, [(64, 4)] * 2, 2, 32)     # warm-up
-    res = {"workload": f"llama13b-{args.layers}layers-bf16", "command":
+    res = {"workload": f"llama13b-{args.layers}layers-bf16" + (f"-kv-{args.kv8}" if args.kv8 else ""), "command":
            "python -m paper_2308_16369_amd.serve " + " ".join(argv if argv is not None else sys.argv[1:]),
            "note": f"{n_req} requests of equal P and D per run, B = {args.batch} resident at once; baseline = "
                    f"whole-prompt prefill-only iterations then decode-only iterations (Sec. 5.1); synthetic "

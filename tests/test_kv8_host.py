@@ -179,3 +179,83 @@ def test_oracle_attend():
     assert np.allclose(o, v.mean(0)) and np.allclose(a, o) and mag == 0
     o, _, _ = ref.attend(np.array([100.0, 0, 0]), np.eye(4)[:, :3], v, 1.0)
     assert np.allclose(o, v[0])
+
+
+# ---------------------------------------------------------------------------- decoder layer
+
+def layer_args(lib, **kw):
+    kv_cfg = cfg(rope_dim=64)
+    model = S.make_cfg(128, 8, 64, 256, n_layers=2)
+    kv = S.sarathi_kv8_alloc(kv_cfg, 4, 128, FAKE, S.sarathi_kv8_bytes(kv_cfg, 4, 128))
+    b, keep = S.make_mixed_batch([(0, 0, 8)], [1], [5])
+    ws = S.sarathi_kv8_workspace_bytes(model, kv_cfg, 9, 1, 128)
+    names = ["norm1_g", "w_qkv", "w_o", "norm2_g", "w_up", "w_down"]
+    w = S.make_kv8_weights({n: FAKE for n in names})
+    args = dict(cfg=ct.byref(model), w=ct.byref(w), kv=kv.handle, layer=0, batch=ct.byref(b), x=FAKE, y=FAKE + (1 << 20),
+                ws=FAKE + (4 << 20), size=ws)
+    args.update(kw)
+    return args, (kv_cfg, model, kv, b, keep, w)
+
+
+def test_layer_workspace(lib):
+    kv_cfg, model = cfg(rope_dim=64), S.make_cfg(128, 8, 64, 256, n_layers=2)
+    n = S.sarathi_kv8_workspace_bytes(model, kv_cfg, 9, 1, 128)
+    L = S.sarathi_kv8_workspace_layout(model, kv_cfg, 9, 1, 128)
+    assert L.total == n > 0 and [L.a, L.qkv, L.o, L.hres, L.m] == sorted([L.a, L.qkv, L.o, L.hres, L.m])
+    assert L.o - L.qkv >= 9 * (8 + 2 * 2) * 64 * 2
+    for other in (S.make_cfg(128, 4, 64, 256, n_layers=2), S.make_cfg(128, 8, 128, 256, n_layers=2),
+                  S.make_cfg(128, 8, 64, 256, n_layers=3), S.make_cfg(128, 8, 64, 256, n_layers=2, dtype=S.F32),
+                  S.make_cfg(128, 8, 64, 256, n_layers=2, rope=0),
+                  S.make_cfg(128, 8, 64, 256, n_layers=2, rope_base=500000.0)):
+        assert S.sarathi_kv8_workspace_bytes(other, kv_cfg, 9, 1, 128) == 0
+        with pytest.raises(S.SarathiError):
+            S.sarathi_kv8_workspace_layout(other, kv_cfg, 9, 1, 128)
+    for bad in ((0, 1, 128), (9, -1, 128), (9, 1, 0)):
+        assert S.sarathi_kv8_workspace_bytes(model, kv_cfg, *bad) == 0
+
+
+def test_layer_refuses(lib):
+    def call(step=False, **kw):
+        a, keep = layer_args(lib, **kw)
+        if step:
+            return lib.sarathi_kv8_model_step(a["cfg"], a["w"], a["kv"], a["batch"], a["x"], a["y"], a["ws"], a["size"], None)
+        return lib.sarathi_kv8_layer_forward(a["cfg"], a["w"], a["kv"], a["layer"], a["batch"], a["x"], a["y"], a["ws"],
+                                             a["size"], None)
+
+    a, keep = layer_args(lib)
+    no_w = S.make_kv8_weights({"norm1_g": FAKE})
+    off = S.make_kv8_weights({n: FAKE + 4 for n in ("norm1_g", "w_qkv", "w_o", "norm2_g", "w_up", "w_down")})
+    other = S.make_cfg(128, 4, 64, 256, n_layers=2)
+    empty = S.sarathi_mixed_batch(0, None, None, None, 0, None, None)
+    for kw in (dict(cfg=None), dict(w=None), dict(kv=None), dict(layer=2), dict(layer=-1), dict(batch=None), dict(x=None),
+               dict(y=None), dict(ws=None), dict(x=FAKE + 2), dict(ws=FAKE + (4 << 20) + 8), dict(y=FAKE),
+               dict(y=FAKE + (4 << 20)), dict(x=FAKE + (4 << 20) + 64), dict(w=ct.byref(no_w)), dict(w=ct.byref(off)),
+               dict(cfg=ct.byref(other)), dict(batch=ct.byref(empty))):
+        assert call(**kw) == S.EINVAL, kw
+    assert call(size=a["size"] - 1) == S.ENOSPC
+    ws2 = (S.sarathi_kv8_layer_weights * 2)(keep[5], no_w)      # the second layer's weights are missing
+    assert call(step=True, w=ws2) == S.EINVAL
+    far, keep2 = S.make_mixed_batch([(0, 125, 8)], [], [])
+    assert call(batch=ct.byref(far)) == S.ERANGE
+
+
+def test_layer_needs_gains_with_norms(lib):
+    kv_cfg = cfg(rope_dim=64, qk_norm=1)
+    kv = S.sarathi_kv8_alloc(kv_cfg, 4, 128, FAKE, S.sarathi_kv8_bytes(kv_cfg, 4, 128))
+    names = ["norm1_g", "w_qkv", "w_o", "norm2_g", "w_up", "w_down"]
+    for extra in ({}, {"q_gain": FAKE}, {"q_gain": FAKE, "k_gain": FAKE + 2}):
+        w = S.make_kv8_weights({**{n: FAKE for n in names}, **extra})
+        a, keep = layer_args(lib, w=ct.byref(w), kv=kv.handle)
+        assert lib.sarathi_kv8_layer_forward(a["cfg"], a["w"], a["kv"], 0, a["batch"], a["x"], a["y"], a["ws"], a["size"],
+                                             None) == S.EINVAL
+        assert "gain" in S.sarathi_last_error()
+
+
+def test_serving_equation_counts_the_smaller_cache():
+    import workloads as wl
+    from paper_2308_16369_amd import serve
+
+    shape, mem = wl.LLAMA13B_LAYER.shape, 288 * 10 ** 9
+    full, half = (serve.equation_batch(shape, 40, 1024, mem, kv8_block=b) for b in (0, 64))
+    assert half["kv_bytes_per_token"] == 40 * 2 * 40 * (128 + 4 / 64)
+    assert 1.99 * full["B"] <= half["B"] + 1 <= 2 * full["B"] + 2
