@@ -175,10 +175,11 @@ __device__ __forceinline__ float scale_of(float top) {
 }
 
 // Eight codes of x * inv, |x * inv| at most the largest code but for the last
-// bits, which the rounding takes away.  int8: adding 1.5 2^23 rounds to the
-// nearest whole number (ties to even), which the sum's low byte then is.
+// bits, which the rounding takes away.  int8: adding 1.5 2^23 rounds the product
+// to the nearest whole number (ties to even), which the sum's low byte then is.
 template <bool INT8>
 __device__ __forceinline__ uint2 encode8(const float* x, float inv) {
+#pragma clang fp contract(off)
   uint32_t w[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -186,7 +187,7 @@ __device__ __forceinline__ uint2 encode8(const float* x, float inv) {
     if constexpr (INT8) {
       uint32_t b[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(fmaf(y[e], inv, 12582912.f));
+      for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(y[e] * inv + 12582912.f);
       w[h] = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400) | __builtin_amdgcn_perm(b[3], b[2], 0x04000c0c);
     } else {
       const int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, 0, false);
