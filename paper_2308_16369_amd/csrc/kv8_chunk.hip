@@ -11,15 +11,17 @@
 //   reads.  A scale is constant over 16 keys: the key scale joins the softmax
 //   scale in the exponent, the value scale enters there as its logarithm (the
 //   row sum divides it out again), so neither costs a multiplication per score.
-// 512 rows over a prefix of 2048 (52 heads): 56 us, 0.56 PFLOP/s; a 4096-token
-// prompt (32 / 8 heads): 178 us, 0.77 PFLOP/s.  A wave's tile takes 4800 cycles
-// alone on its SIMD and 5150 beside another's, of which the matrix cores are
-// busy 1024: it is bound by the latency of its own chain (LDS reads, products,
-// maximum, exponentials, products, staging, barrier).  Tried and no faster:
-// the next tile's products under this one's exponentials, fragments read ahead
-// into registers, 32-key tiles with three waves per SIMD, 64 rows per wave (the
-// accumulators then move between register files), and operands straight from
-// global memory (440 us for the prompt).
+// 512 rows over a prefix of 2048 (52 heads): 54 us, 0.59 PFLOP/s; a 4096-token
+// prompt (32 / 8 heads): 179 us, 0.77 PFLOP/s.  A wave's tile takes some 4700
+// cycles, of which the matrix cores are busy 1024: it is bound by the latency of
+// its own chain (LDS reads, products, maximum, exponentials, products, barrier).
+// Fragments are therefore read a step ahead of their products and the next
+// tile is converted and stored beside the second products; either alone gains
+// 0 to 1 %, both together 6 % on the first case and 2 % on the second.  Tried
+// and no faster: the next tile's products under this one's exponentials, 32-key
+// tiles with three waves per SIMD, 64 rows per wave (the accumulators then move
+// between register files), and operands straight from global memory (440 us for
+// the prompt).
 #include "kv8_device.h"
 
 namespace sarathi {
@@ -158,18 +160,17 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
       vr[i] = *reinterpret_cast<const uint4*>(vp + off);
     }
   };
-  auto stage = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int r = sr + i * (256 / LPR);
-      u32x4 lo, hi;
-      widen16<INT8>(kr[i], lo, hi);
-      ring[2 * buf * TILE + r * DCH + swz<D>(2 * sc, r)] = lo;
-      ring[2 * buf * TILE + r * DCH + swz<D>(2 * sc + 1, r)] = hi;
-      widen16<INT8>(vr[i], lo, hi);
-      ring[(2 * buf + 1) * TILE + r * DCH + swz<D>(2 * sc, r)] = lo;
-      ring[(2 * buf + 1) * TILE + r * DCH + swz<D>(2 * sc + 1, r)] = hi;
-    }
+  auto stage_piece = [&](u32x4* tile, const uint4& x, int i) {
+    const int r = sr + i * (256 / LPR);
+    u32x4 lo, hi;
+    widen16<INT8>(x, lo, hi);
+    tile[r * DCH + swz<D>(2 * sc, r)] = lo;
+    tile[r * DCH + swz<D>(2 * sc + 1, r)] = hi;
+  };
+  // piece j of the fetched tile (its NI pieces of K, then those of V)
+  auto stage = [&](int buf, int j) {
+    if (j < NI) stage_piece(ring + 2 * buf * TILE, kr[j % NI], j);
+    else if (j < 2 * NI) stage_piece(ring + (2 * buf + 1) * TILE, vr[j % NI], j - NI);
   };
 
   // transposed-read offsets of V^T fragments (rows 4 g + e and + 8 of a 16-key step)
@@ -190,19 +191,48 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
   float ks4[4], vs4[4];
   auto compute = [&](int it, int buf) {
     const int k0 = kbeg + (NG * it + grp) * KT;
-    if (k0 > last_key || k0 >= kend || idle) return;
-    floatx16 s[2];
+    if (k0 > last_key || k0 >= kend || idle) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+      for (int j = 0; j < 2 * NI; ++j) stage(buf ^ 1, j);
+      return;
+    }
+    // Fragments are read a step ahead of their products (the scheduling barriers
+    // keep them there: left alone, the compiler saves registers by waiting for
+    // every read just before its product, 16 LDS latencies in a row).
+    floatx16 s[2];
+    bf16x8_t kf[2][4];
+    auto read_k = [&](bf16x8_t* f, int i) {                 // step i: 16-dim slices 2 i, 2 i + 1 of both halves
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        f[e] = __builtin_bit_cast(bf16x8_t, ring[2 * buf * TILE + (e & 1) * 32 * DCH + koff[2 * i + (e >> 1)]]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+    read_k(kf[0], 0);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, ring[2 * buf * TILE + kb * 32 * DCH + koff[ks]]);
+    for (int i = 0; i < D / 32; ++i) {
+      if (i + 1 < D / 32) read_k(kf[(i + 1) & 1], i + 1);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][n], s[kb], 0, 0, 0);
-      }
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          s[e & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 1][e], qf[2 * i + (e >> 1)][n], s[e & 1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    // V^T of a 16-key step
+    const char* vt = reinterpret_cast<const char*>(ring + (2 * buf + 1) * TILE);
+    bf16x8_t vf[2][D / 32];
+    auto read_v = [&](bf16x8_t* f, int i) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const uint2 x = lds_tr16(vt + voff[0][db] + i * 16 * DCH * 16), y = lds_tr16(vt + voff[1][db] + i * 16 * DCH * 16);
+        f[db] = __builtin_bit_cast(bf16x8_t, u32x4{x.x, x.y, y.x, y.y});
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
     const bool full = k0 + KT <= kend && k0 + KT - 1 <= offset + r0 + wave * 32 / group;
     if (!full) {
       const int lim = min(qpos, kend - 1) - k0;
@@ -230,17 +260,16 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
       m_run = m_new;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
-    bf16x8_t pf[4][NT];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    bf16x8_t pf[2][NT];
+    auto probs = [&](bf16x8_t* f, int i) {
       const float add = __builtin_amdgcn_logf(vs4[i]) - m_use;   // log2
       float p[8], sum = 0.f;
 #pragma unroll
       for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][8 * (i & 1) + v], ks4[i], add));
-      split8<NT>(p, pf[i]);
+      split8<NT>(p, f);
       if constexpr (NT == 1) {
         // the row sum takes the rounded probabilities that multiply V
-        const u32x4 w = __builtin_bit_cast(u32x4, pf[i][0]);
+        const u32x4 w = __builtin_bit_cast(u32x4, f[0]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t pair = w[e];
@@ -251,18 +280,21 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
         for (int v = 0; v < 8; ++v) sum += p[v];
       }
       l_run = fmaf(sum, __builtin_amdgcn_rcpf(vs4[i]), l_run);
-    }
-    const char* vt = reinterpret_cast<const char*>(ring + (2 * buf + 1) * TILE);
+    };
+    read_v(vf[0], 0);
+    probs(pf[0], 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      if (i < 3) read_v(vf[(i + 1) & 1], i + 1);
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        const uint2 x = lds_tr16(vt + voff[0][db] + i * 16 * DCH * 16), y = lds_tr16(vt + voff[1][db] + i * 16 * DCH * 16);
-        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, u32x4{x.x, x.y, y.x, y.y});
+      for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[i][n], o_acc[db], 0, 0, 0);
-      }
+          o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i & 1][db], pf[i & 1][n], o_acc[db], 0, 0, 0);
+      stage(buf ^ 1, i);                                        // the next tile's codes, beside the products
+      if (i < 3) probs(pf[(i + 1) & 1], i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   auto step = [&](int it, int buf) {
@@ -273,12 +305,12 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
       vs4[i] = vs_next[i] > 0.f ? vs_next[i] : 1.f;
     }
     if (it + 1 < n_iter) fetch(it + 1);
-    compute(it, buf);
-    if (it + 1 < n_iter) stage(buf ^ 1);
+    compute(it, buf);                      // (the last tile stages itself again, unread)
     __syncthreads();
   };
   fetch(0);
-  stage(0);
+#pragma unroll
+  for (int j = 0; j < 2 * NI; ++j) stage(0, j);
   __syncthreads();
   for (int it = 0; it < n_iter; it += 2) {
     step(it, 0);
