@@ -153,7 +153,13 @@ int sarathi_kv8_append(const sarathi_kv8_plan* plan, int layer, const void* qkv,
  * Scores, softmax and sums in fp32; products on the matrix cores from the
  * codes, which are exact in bf16: bf16 rows multiply as they are, with the
  * probabilities (times the value scale) rounded to bf16; fp32 rows and their
- * probabilities go in as three bf16 terms each (24 bits).
+ * probabilities go in as three bf16 terms each (24 bits).  Decodes of bf16 rows
+ * over int8 codes multiply in f16 instead: q by a power of two per head (its
+ * elements keep their 8 bits down to 2^-28 of the head's largest; a head with a
+ * magnitude beyond 2^111 gives NaN), the probabilities (times the value scale)
+ * with 11 bits, and dropped below 2^-32 of the largest; sums take the codes as
+ * code + 128, so their fp32 roundings are relative to 128 scales, not to the
+ * values (some 2^-24 of a block's largest magnitude each).
  * out [T, ld_out] must not overlap q.
  * Errors: EINVAL (NULL, layer, alignment, overlap), EHIP.
  */

@@ -118,8 +118,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
 
   // m_run: the running maximum of head c's scores (the same in its four lanes),
   // l_run: this lane's share of the row sum, in units of 2^m_run.  F16: M_run,
-  // the running maximum of score + log2(value scale); o and lp (the sum of the
-  // rounded probabilities) are in units of 2^M_run.
+  // the running maximum of score + log2(value scale) - 7; o and lp (the sum of
+  // the rounded probabilities) are in units of 2^M_run.  The 7 puts the
+  // probabilities (at most 2^15) at the top of f16's range: they keep 11 bits
+  // down to 2^-21 of the largest and are dropped below 2^-32.
   float m_run = -INFINITY, M_run = -INFINITY, l_run = 0.f, lp = 0.f;
   floatx4 o[DB];
 #pragma unroll
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
     if constexpr (F16) {
       // value scales as logarithms; a zero scale belongs to zero codes: any small one does
       const float lv0 = __builtin_amdgcn_logf(fmaxf(t.vs[0], KV8_TINY)), lv1 = __builtin_amdgcn_logf(fmaxf(t.vs[1], KV8_TINY));
-      const float Mx = groups_max(fmaxf(mx0 + lv0, mx1 + lv1));
+      const float Mx = groups_max(fmaxf(mx0 + lv0, mx1 + lv1)) - 7.f;
       if (__ballot(mx > m_run + 8.0f || Mx > M_run + 8.0f)) {
         const float m_new = fmaxf(m_run, mx), M_new = fmaxf(M_run, Mx);
         l_run *= m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
       u32x4 y[4];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = t.v[e][x];
-      transpose8<INT8, F16, 4>(v, y);
+      transpose8<INT8, F16>(v, y);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const u32x4 vf = y[b];
@@ -312,8 +314,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
   }
   l_run = groups_sum(l_run);
   if constexpr (F16) {
-    // o = 2^24 (sum of p u) - 128 (sum of p), and from units of 2^M_run to those
-    // of 2^m_run (m_run -inf: the wave had no keys, all zeros)
+    // o = 2^24 (sum of p u) - 128 (sum of p), and to units of 2^m_run (m_run -inf:
+    // the wave had no keys, all zeros)
     const float bias = 128.f * groups_sum(lp), f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M_run - m_run);
 #pragma unroll
     for (int db = 0; db < DB; ++db)

@@ -9,8 +9,8 @@
 // and alike for V with the sum of the probabilities.  q is scaled by a power of
 // two into f16's range (its 8 bits fit; elements below 2^-28 of the row's
 // largest lose bits, rows beyond 2^111 become NaN), and the probabilities times
-// their value scale are kept near one by a running maximum of their own (the
-// scales may differ by any factor), so they keep 11 bits.
+// their value scale are kept at the top of f16's range by a running maximum of
+// their own (the scales may differ by any factor), so they keep 11 bits.
 #pragma once
 
 #include "kv8.h"
@@ -82,24 +82,22 @@ __device__ __forceinline__ f16x8_t codes8_f16(uint32_t a, uint32_t b) {
                                             __builtin_amdgcn_perm(y, y, 0x0c010c00), __builtin_amdgcn_perm(y, y, 0x0c030c02)}));
 }
 // Byte b of eight keys' dwords as one operand (the keys along its eight elements).
-template <bool INT8, bool F16, int NB>
+template <bool INT8, bool F16>
 __device__ __forceinline__ void transpose8(const uint32_t* v, u32x4* y) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if constexpr (F16) {
       const uint32_t w0 = offset_codes(v[2 * e]), w1 = offset_codes(v[2 * e + 1]);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) y[b][e] = __builtin_amdgcn_perm(w1, w0, 0x0c040c00 + 0x00010001 * b);
+      for (int b = 0; b < 4; ++b) y[b][e] = __builtin_amdgcn_perm(w1, w0, 0x0c040c00 + 0x00010001 * b);
     } else {
       uint32_t lo0, hi0, lo1, hi1;
       codes_bf16<INT8>(v[2 * e], lo0, hi0);
       codes_bf16<INT8>(v[2 * e + 1], lo1, hi1);
       y[0][e] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100);
       y[1][e] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302);
-      if constexpr (NB == 4) {
-        y[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
-        y[3][e] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302);
-      }
+      y[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
+      y[3][e] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302);
     }
   }
 }

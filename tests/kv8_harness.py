@@ -214,14 +214,30 @@ def check_append(spec: Spec, batch: Batch, before, after, q_out, q, k, v, layer=
     assert np.all(same[~touched_s])
 
 
-def check_attention(spec: Spec, batch: Batch, values, q, out, layer=0):
+def offset_error(spec: Spec, batch: Batch, row, scales, w):
+    """What the offset of the codes adds to the tolerance of a decode of bf16 rows over int8 codes, from weights w.
+
+    The kernel sums p_j u_j (u = code + 128 <= 255) in fp32 and takes 128 sum(p)
+    out again.  Of n keys a wave sums n / 4 in steps of 32: 32 products and the
+    sum so far, each added with an error of at most 2^-23 (truncation) of a sum
+    that 255 sum(p) bounds; the sum of the p's takes 8 more of a bound half as
+    large, the merge 4: below 40 ceil(n / 128) 2^-23 255 in codes, times the
+    weights and their scales."""
+    if spec.dtype != "bf16" or spec.fmt != "int8" or row < batch.T - len(batch.decodes):
+        return 0.0
+    n = len(w)
+    return 40 * -(-n // 128) * 2.0 ** -23 * 255 * float(w @ np.repeat(scales, spec.block)[:n])
+
+
+def check_attention(spec: Spec, batch: Batch, values, q, out, layer=0, scales=None):
     """Outputs against float64 over the cache's own values.
 
     Tolerances, of the weighted sum A = sum_j w_j |v_j|.  Scores: 2 D + 8
     fp32 roundings of sum |q k| (three times the products in fp32 rows), an
     exponent and its argument (|s| 2^-23): a relative error of every weight,
     twice (numerator and row sum).  bf16 rows: the probabilities' rounding,
-    2^-8, twice, and the output's own."""
+    2^-8, twice, and the output's own.  With scales (of the cache): the codes'
+    offset as well, for inputs whose heavy keys have small values."""
     scale = spec.softmax_scale or 1 / math.sqrt(spec.dim)
     qv, ov = f64(q).reshape(-1, spec.heads, spec.dim), f64(out).reshape(-1, spec.heads, spec.dim)
     worst = 0.0
@@ -232,6 +248,11 @@ def check_attention(spec: Spec, batch: Batch, values, q, out, layer=0):
             terms = 3 if spec.dtype == "f32" else 1
             rel = (2 * spec.dim * terms + 16) * 2.0 ** -24 * max(mag, 1.0) + 2.0 ** -20
             tol = 2 * rel * a + (2 * 2.0 ** -8 * a + 2.0 ** -8 * np.abs(o) if spec.dtype == "bf16" else 2.0 ** -23 * np.abs(o))
+            if scales is not None:
+                sc = scales[layer, slot, :, h // spec.group].astype(np.float64)
+                s = scale * (kv[0] @ qv[r, h])
+                w = np.exp(s - s.max())
+                tol = tol + offset_error(spec, batch, r, sc[1], w / w.sum())
             d = np.abs(ov[r, h] - o)
             assert np.all(d <= tol + 1e-30), (r, h, slot, pos, float(np.max(d / (tol + 1e-30))))
             worst = max(worst, float(np.max(d / (tol + 1e-30))))

@@ -266,6 +266,58 @@ def test_attention_peaked_and_scaled():
         check_attention(spec, b, cache.values(), q, attend(cache, b, q))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_int8_scales_far_apart(dtype):
+    """Value scales 2^60 apart, zero blocks, query heads of magnitude 2^-40 and with one strong element."""
+    spec = Spec(heads=4, kv_heads=2, dim=64, dtype=dtype, fmt="int8", block=32)
+    cache = Cache(spec)
+    cache.fill(gen(43))
+    codes, scales = cache.views()
+    scales[0, 0, 1, :, 1] *= 2.0 ** 60
+    scales[0, 1, 1, :, 2] *= 2.0 ** -60
+    codes[0, 2, :, :, 64:96] = 0
+    scales[0, 2, :, :, 2] = 0
+    b = Batch(chunks=[(0, 40, 90)], decodes=[(1, 200), (3, 299), (2, 250)])
+    q = torch.randn((b.T, 4 * 64), device="cuda", generator=gen(44))
+    q[-2, 64:128] *= 2.0 ** -40
+    q[-1, :64] *= 2.0 ** -20
+    q[-1, 7] = 3.0
+    q = q.to(spec.tdt)
+    check_attention(spec, b, cache.values(), q, attend(cache, b, q))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_small_weights_keep_their_bits(dtype, fmt):
+    """One key outweighs the others 2^22 times and has a zero value: the output is the others' alone."""
+    spec = Spec(heads=2, kv_heads=1, dim=64, dtype=dtype, fmt=fmt, block=16)
+    cache = Cache(spec)
+    cache.fill(gen(45))
+    codes, scales = cache.views()
+    codes[:, :, 0] = 0                                     # keys: zero but the first, of ones
+    codes[:, :, 0, :, 0] = 1 if fmt == "int8" else 0x38
+    codes[:, :, 1, :, 0] = 0                               # its value
+    # q of ones: score 64 scale / sqrt(64) = 22 log 2
+    scales[:, :, 0] = 22 * 0.6931471805599453 / 8
+    b = Batch(chunks=[(1, 60, 70)], decodes=[(0, 31), (2, 299)])
+    q = torch.ones((b.T, 2 * 64), device="cuda", dtype=spec.tdt)
+    check_attention(spec, b, cache.values(), q, attend(cache, b, q), scales=cache.host()[1])
+
+
+@pytest.mark.parametrize("dim,fmt", [(64, "e4m3"), (128, "int8"), (128, "e4m3")])
+def test_attention_many_blocks(dim, fmt):
+    """So many heads times query blocks that a block's keys stay with one group of waves."""
+    spec = Spec(heads=64, kv_heads=64, dim=dim, fmt=fmt, block=64, seq=620, slots=2)
+    cache = Cache(spec)
+    cache.fill(gen(46))
+    b = Batch(chunks=[(1, 11, 600)])
+    poison_unwritten(cache, b)
+    q = torch.randn((b.T, 64 * dim), device="cuda", generator=gen(47)).to(spec.tdt)
+    out, values = attend(cache, b, q), cache.values()
+    for first, n in ((0, 6), (126, 5), (595, 5)):
+        check_attention(spec, Batch(chunks=[(1, 11 + first, n)]), values, q[first:first + n], out[first:first + n])
+
+
 def test_attention_non_finite_rows_stay_alone():
     """A NaN or infinite query row spoils its own output only."""
     spec = Spec(heads=4, kv_heads=2, dim=64, fmt="int8", block=16)
