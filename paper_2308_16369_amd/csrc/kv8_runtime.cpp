@@ -59,6 +59,7 @@ constexpr long DEC_BLOCKS = 768;
 constexpr int PRE_MIN_TILES = 4;
 constexpr long PRE_SPLIT_BLOCKS = 768, PRE_SLOTS = 512;
 constexpr double PRE_FIXED_TILES = 2, PRE_FIXED_TILES_2 = 3, PRE_TILE_2 = 1.15, PRE_JOIN_TILES = 6;
+constexpr int MAX_SLOTS = 1 << 20, MAX_SEQ = 1 << 20;
 constexpr long MAX_GRID = (1l << 24) - 1;   // blocks of 256 threads in one launch
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -155,7 +156,7 @@ PlanLayout plan_layout(const sarathi_kv8_cfg& c, int T, int n_chunks) {
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align256(off + bytes); return at; };
   const int rpb = rows_per_block(c);
-  const long qblocks = T / rpb + n_chunks;
+  const long qblocks = (long)(T / rpb) + n_chunks;
   L.rows = take((size_t)T * 5 * 4);
   L.tab = take((size_t)T * (c.rope_dim / 2) * sizeof(float2));
   // spans and touched blocks have a row at least
@@ -572,8 +573,16 @@ int guarded(F&& f) {
 extern "C" {
 
 size_t sarathi_kv8_bytes(const sarathi_kv8_cfg* cfg, int n_slots, int max_seq_len) {
-  if (check_kv8_cfg(cfg) != SARATHI_OK || n_slots < 1 || max_seq_len < 1) return 0;
-  const sarathi_kv8_layout L = layout_of(*cfg, n_slots, max_seq_len);
+  if (check_kv8_cfg(cfg) != SARATHI_OK) return 0;
+  if (n_slots < 1 || n_slots > MAX_SLOTS || max_seq_len < 1 || max_seq_len > MAX_SEQ) {
+    fail(SARATHI_EINVAL, "n_slots %d or max_seq_len %d out of range", n_slots, max_seq_len);
+    return 0;
+  }
+  const sarathi_kv8_layout L = layout_of(*cfg, n_slots, max_seq_len);   // a layer: below 2^61 bytes
+  if (L.layer > (size_t(1) << 62) / (size_t)cfg->n_layers) {
+    fail(SARATHI_EUNSUPPORTED, "%d layers of %zu bytes", cfg->n_layers, L.layer);
+    return 0;
+  }
   return L.scale_offset + L.scale_layer * cfg->n_layers * sizeof(float);
 }
 
@@ -585,9 +594,10 @@ int sarathi_kv8_alloc(const sarathi_kv8_cfg* cfg, int n_slots, int max_seq_len, 
   *out = nullptr;
   if (!dev_mem) return fail(SARATHI_EINVAL, "dev_mem is NULL");
   if (!aligned16(dev_mem)) return fail(SARATHI_EINVAL, "dev_mem must be 16-byte aligned");
-  if (n_slots < 1 || n_slots > (1 << 20)) return fail(SARATHI_EINVAL, "n_slots %d out of range", n_slots);
-  if (max_seq_len < 1 || max_seq_len > (1 << 20)) return fail(SARATHI_EINVAL, "max_seq_len %d out of range", max_seq_len);
+  if (n_slots < 1 || n_slots > MAX_SLOTS) return fail(SARATHI_EINVAL, "n_slots %d out of range", n_slots);
+  if (max_seq_len < 1 || max_seq_len > MAX_SEQ) return fail(SARATHI_EINVAL, "max_seq_len %d out of range", max_seq_len);
   const size_t need = sarathi_kv8_bytes(cfg, n_slots, max_seq_len);
+  if (need == 0) return SARATHI_EUNSUPPORTED;   // more bytes than can be addressed
   if (dev_bytes < need) return fail(SARATHI_ENOSPC, "KV memory of %zu bytes < %zu needed", dev_bytes, need);
   sarathi_kv8* kv = new (std::nothrow) sarathi_kv8{};
   if (!kv) return fail(SARATHI_ENOSPC, "out of host memory");

@@ -74,6 +74,15 @@ def test_alloc_refuses(lib):
     lib.sarathi_kv8_plan_free(None)
 
 
+def test_sizes_beyond_addressing(lib):
+    """Sizes whose product passes 64 bits are refused, never wrapped."""
+    c, h = cfg(n_heads=4096, n_kv_heads=4096, head_dim=128, n_layers=64), ct.c_void_p()
+    assert S.sarathi_kv8_bytes(c, 1 << 20, 1 << 20) == 0
+    assert lib.sarathi_kv8_alloc(ct.byref(c), 1 << 20, 1 << 20, FAKE, (1 << 64) - 1, ct.byref(h)) == S.EUNSUPPORTED and not h
+    assert S.sarathi_kv8_bytes(c, (1 << 20) + 1, 64) == 0 and S.sarathi_kv8_bytes(c, 64, (1 << 20) + 1) == 0
+    assert S.sarathi_kv8_plan_bytes(cfg(), (1 << 31) - 1, (1 << 31) - 1, 64) > (1 << 40)
+
+
 BAD_BATCH = [
     ([], [], [], S.EINVAL), ([(4, 0, 1)], [], [], S.EINVAL), ([(-1, 0, 1)], [], [], S.EINVAL),
     ([(0, -1, 4)], [], [], S.ERANGE), ([(0, 0, 0)], [], [], S.ERANGE), ([(0, 100, 29)], [], [], S.ERANGE),
