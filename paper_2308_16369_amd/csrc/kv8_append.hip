@@ -5,8 +5,10 @@
 namespace sarathi {
 
 // ------------------------------------------------------------------ a plan's rows
-// One block per span.  The angles in fp64, reduced to [-pi, pi], then fp32 sine
-// and cosine; made once for a batch and read by every layer's append.
+// One block per span.  Angles, sines and cosines in fp64, rounded once: a sine
+// of the angle rounded to fp32 is off by up to 2^-23 more, and rows near the
+// middle of two codes then take the other one.  Made once for a batch and read
+// by every layer's append.
 __global__ __launch_bounds__(256) void kv8_rows_kernel(Kv8RowsArgs a) {
   const int* sp = a.spans + KV8_SPAN_INTS * blockIdx.x;
   const int slot = sp[0], pos = sp[1], row = sp[2], n = sp[3], part = sp[4], ns = sp[5], stride = sp[6];
@@ -22,9 +24,9 @@ __global__ __launch_bounds__(256) void kv8_rows_kernel(Kv8RowsArgs a) {
     const int j = t / a.pairs, i = t - j * a.pairs;
     const double ang = (double)(pos + j) * a.theta[i];
     const double red = ang - 6.283185307179586 * rint(ang * 0.15915494309189535);
-    float sn, cs;
-    sincosf((float)red, &sn, &cs);
-    a.tab[(size_t)(row + j) * a.pairs + i] = make_float2(cs * a.mscale, sn * a.mscale);
+    double sn, cs;
+    sincos(red, &sn, &cs);
+    a.tab[(size_t)(row + j) * a.pairs + i] = make_float2((float)(cs * a.mscale), (float)(sn * a.mscale));
   }
 }
 

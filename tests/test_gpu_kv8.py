@@ -107,6 +107,20 @@ def test_append_far_positions():
         assert np.all(err <= 0.5 * st.T[:, :, None] + 2.0 ** -18 * np.abs(want).max())
 
 
+def test_append_sines_are_rounded_once():
+    """fp32 heads of ones and zeros turn into the table's cosines and sines: half a step from the float64 ones (and
+    the float64 angle's own roundings: three of a half 2^-52 of up to 2100 radians, below 1e-12)."""
+    spec = Spec(heads=1, kv_heads=1, dim=128, dtype="f32", rot=128, layout="interleaved", slots=2, seq=2100)
+    cache = Cache(spec)
+    b = Batch(chunks=[(0, 0, 2099)], decodes=[(1, 1777)])
+    qkv = torch.zeros((b.T, 3 * 128), device="cuda")
+    qkv[:, 0:128:2] = 1
+    q = f64(append(cache, b, qkv, [qkv, qkv]))
+    ang = np.array([p for _, p in b.rows()], dtype=np.float64)[:, None] * np.asarray(spec.thetas())
+    for got, want in ((q[:, 0::2], np.cos(ang)), (q[:, 1::2], np.sin(ang))):
+        assert np.all(np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + 1e-12)
+
+
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_append_non_finite_zero_and_tiny(fmt):
     """Infinities become the largest code, NaN zero, neither moves the scale; zero and tiny blocks have scale 0."""
