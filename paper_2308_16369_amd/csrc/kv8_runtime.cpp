@@ -196,9 +196,10 @@ void plan_chunks(const sarathi_kv8_cfg& c, const BatchDesc& b, HostPlan* p) {
   // choice that ends first: the longest range or the rounds of average ones,
   // with a block's set-up and output, and the combine pass where rows are split.
   // Two groups finish a block in about half the time without splitting its rows:
-  // 512 rows over 2048 keys of 52 heads (208 blocks) take 58 us, one group 73,
-  // one group with rows split in two 65; a 4096-token prompt of 32 / 8 heads
-  // (1024 blocks), which fills the GPU either way, 196 against 187 of one group.
+  // 512 rows over 2048 keys of 52 heads (208 blocks) take 54 us, one group with
+  // rows split in two 64; three prompts of 347 to 910 rows of 32 / 8 heads 48
+  // against 61; a 4096-token prompt of 32 / 8 heads (1024 blocks), which fills
+  // the GPU either way, 189 against 179 of one group.
   int tau = longest;
   double best = 1e300;
   for (int groups = 1; groups <= (c.dtype == SARATHI_BF16 ? 2 : 1); ++groups) {
