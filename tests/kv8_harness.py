@@ -124,7 +124,10 @@ class Cache:
         size = S.sarathi_kv8_plan_bytes(self.c, rows, n, self.spec.seq)
         ws = torch.full((size + GUARD,), 255, dtype=torch.uint8, device="cuda")
         b, keep = S.make_mixed_batch(list(batch.chunks), [d[0] for d in batch.decodes], [d[1] for d in batch.decodes])
-        stream = torch.cuda.current_stream().cuda_stream if stream is None else stream
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        else:
+            torch.cuda.synchronize()           # the fill runs on the current stream, the upload on another
         p = S.sarathi_kv8_plan_create(self.kv, b, ws.data_ptr(), size, stream)
         p.ws = ws
         return p
