@@ -438,14 +438,15 @@ LayerLayout layer_layout(const sarathi_model_cfg& c, const sarathi_kv8_cfg& k, i
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align256(off + bytes); return at; };
   const size_t es = esize(c.dtype), H = c.hidden, hd = k.head_dim;
-  L.a = take(T * H * es);
-  L.qkv = take(T * (k.n_heads + 2 * (size_t)k.n_kv_heads) * hd * es);
-  L.o = take(T * k.n_heads * hd * es);
-  L.hres = take(T * H * 4);
-  L.m = take(T * (size_t)c.ffn * es);
+  const size_t rows = T, nh = k.n_heads;
+  L.a = take(rows * H * es);
+  L.qkv = take(rows * (nh + 2 * (size_t)k.n_kv_heads) * hd * es);
+  L.o = take(rows * nh * hd * es);
+  L.hres = take(rows * H * 4);
+  L.m = take(rows * c.ffn * es);
   L.parts = take((size_t)MAX_SPLIT * std::min(T, PARTS_ROWS) * H * 4);
-  L.ping0 = take(T * H * es);
-  L.ping1 = take(T * H * es);
+  L.ping0 = take(rows * H * es);
+  L.ping1 = take(rows * H * es);
   L.plan = take(plan_layout(k, T, n_chunks).total);
   L.total = off;
   return L;
