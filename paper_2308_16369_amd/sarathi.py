@@ -545,6 +545,8 @@ def sarathi_kv8_layer_forward(cfg, weights: sarathi_kv8_layer_weights, kv: KV8, 
 
 def sarathi_kv8_model_step(cfg, weights: Sequence[sarathi_kv8_layer_weights], kv: KV8, batch, x_in: int, x_out: int,
                            ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
+    if len(weights) < cfg.n_layers:      # the library reads n_layers entries
+        raise SarathiError(EINVAL, f"weights of {len(weights)} layers, the model has {cfg.n_layers}")
     arr = (sarathi_kv8_layer_weights * len(weights))(*weights)
     rc = lib().sarathi_kv8_model_step(ct.byref(cfg), arr, kv.handle, ct.byref(batch), x_in, x_out, ws, ws_bytes, stream)
     return _check(rc) if check else rc
