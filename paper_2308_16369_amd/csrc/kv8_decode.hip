@@ -214,7 +214,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
     uint32_t w[4];
     bf16x8_t pf[NT];
     if constexpr (F16) {
-      // value scales as logarithms; a zero scale belongs to zero codes: any small one does
+      // value scales as logarithms; a zero scale belongs to zero codes: any small one does for the products
       const float lv0 = __builtin_amdgcn_logf(fmaxf(t.vs[0], KV8_TINY)), lv1 = __builtin_amdgcn_logf(fmaxf(t.vs[1], KV8_TINY));
       const float Mx = groups_max(fmaxf(mx0 + lv0, mx1 + lv1)) - 7.f;
       if (__ballot(mx > m_run + 8.0f || Mx > M_run + 8.0f)) {
@@ -228,14 +228,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         M_run = M_new;
       }
       const float d = M_run - m_run;
+      // a group's probabilities are 2^(lv - d) of its weights.  Where that may take weights that count
+      // (down to 2^-66) below fp32's range, the row sum takes them by themselves.
+      const bool apart = __ballot(d - lv0 > 60.f || d - lv1 > 60.f) != 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float lv = h ? lv1 : lv0, add = lv - M_run;
         float p[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) p[v] = __builtin_amdgcn_exp2f(s[h][v] + add);
-        // back to units of 2^m_run and no value scale
-        l_run = fmaf((p[0] + p[1]) + (p[2] + p[3]), __builtin_amdgcn_exp2f(fminf(d - lv, 126.f)), l_run);
+        if (apart) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) l_run += __builtin_amdgcn_exp2f(s[h][v] - m_run);
+        } else {                           // back to units of 2^m_run and no value scale
+          l_run = fmaf((p[0] + p[1]) + (p[2] + p[3]), __builtin_amdgcn_exp2f(d - lv), l_run);
+        }
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           const uint32_t pair = pk_f16(p[2 * v], p[2 * v + 1]);

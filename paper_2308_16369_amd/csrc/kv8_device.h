@@ -10,7 +10,9 @@
 // two into f16's range (its 8 bits fit; elements below 2^-28 of the row's
 // largest lose bits, rows beyond 2^111 become NaN), and the probabilities times
 // their value scale are kept at the top of f16's range by a running maximum of
-// their own (the scales may differ by any factor), so they keep 11 bits.
+// their own, so they keep 11 bits; the row sum, which the value scales have no
+// part in, is taken from the weights themselves where the scales lie so far
+// apart that these products would lose weights.
 #pragma once
 
 #include "kv8.h"
