@@ -159,7 +159,8 @@ int sarathi_kv8_append(const sarathi_kv8_plan* plan, int layer, const void* qkv,
  * magnitude beyond 2^111 gives NaN), the probabilities (times the value scale)
  * with 11 bits, and dropped below 2^-32 of the largest; sums take the codes as
  * code + 128, so their fp32 roundings are relative to 128 scales, not to the
- * values (some 2^-24 of a block's largest magnitude each).
+ * values; the 128 is taken out every 512 keys of a sum, which bounds these
+ * roundings by 2^-10 of a code, whatever the number of keys.
  * out [T, ld_out] must not overlap q.
  * Errors: EINVAL (NULL, layer, alignment, overlap), EHIP.
  */

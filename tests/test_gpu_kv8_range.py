@@ -1,10 +1,12 @@
-"""8-bit KV cache, attention at the ends of its range: value scales far apart and beside zero blocks."""
+"""8-bit KV cache, attention at the ends of its range: value scales far apart and beside zero blocks, very long work
+items."""
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from kv8_harness import Batch, Cache, Spec, check_attention  # noqa: E402
+from kv8_harness import Batch, Cache, Spec, check_attention, cur  # noqa: E402
+from paper_2308_16369_amd import sarathi as S  # noqa: E402
 from test_gpu_kv8 import attend, gen  # noqa: E402
 
 KINDS = [("bf16", "int8"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "e4m3")]
@@ -34,3 +36,39 @@ def test_keys_count_whatever_their_value_scale(dtype, fmt, block, run, first, bi
     b = Batch(chunks=[(1, 37, 70)], decodes=[(0, 299), (2, 47), (3, 160)])
     q = torch.randn((b.T, 4 * 64), device="cuda", generator=gen(4)).to(spec.tdt)
     check_attention(spec, b, cache.values(), q, attend(cache, b, q), scales=cache.host()[1])
+
+
+@pytest.mark.parametrize("n", [20000, 131072, 1 << 20])
+def test_error_does_not_grow_with_the_keys_of_an_item(n):
+    """int8 decodes of n keys in one item each.  The keys come in pairs of equal keys and opposite values, so that the
+    output is the error, in codes (the scale is 1).
+
+    The sums take the codes plus 128 (at most 255).  A correction every 16 steps of 32 keys: a product of 32 keys is
+    added with an error of at most 2^-23 (truncation) of a sum that 255 sum(p) bounds, 2^-23 255 (32 + 64 + .. + 512)
+    / 512 = 2.6e-4 codes; the sum of the probabilities takes four additions a step, 64 2^-23 128 / 2 = 4.9e-4.  The
+    weights' roundings are independent, at most 2^-11 of each, uniform: of codes of rms 73.6 and weights of relative
+    variance exp(0.25), eight standard deviations of the mean are 8 2^-11 73.6 1.13 / sqrt(3 n) = 0.19 / sqrt(n)."""
+    spec = Spec(heads=4096, kv_heads=32, dim=64, dtype="bf16", fmt="int8", block=128, slots=3, seq=n)
+    c = spec.cfg()
+    size = S.sarathi_kv8_bytes(c, 3, n)
+    mem = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    kv = S.sarathi_kv8_alloc(c, 3, n, mem.data_ptr(), size)
+    lay = kv.layout()
+    g = gen(7)
+    k, v = torch.randint(-127, 128, (2, n // 2, 64), device="cuda", generator=g).to(torch.int8)
+    order = torch.randperm(n, device="cuda", generator=g)
+    codes = mem[:3 * 2 * 32 * n * 64].view(torch.int8).view(3, 2, 32, n, 64)
+    codes[:, 0] = torch.cat([k, k])[order]
+    codes[:, 1] = torch.cat([v, -v])[order]
+    at = lay.scale_offset
+    scales = mem[at:at + 4 * 3 * 2 * 32 * lay.scale_head].view(torch.float32).view(3, 2, 32, lay.scale_head)
+    scales[:, 0], scales[:, 1] = 0.007, 1.0
+    mb, keep = S.make_mixed_batch([], [0, 1, 2], [n - 1] * 3)
+    wsz = S.sarathi_kv8_plan_bytes(c, 3, 0, n)
+    ws = torch.empty(wsz, dtype=torch.uint8, device="cuda")
+    plan = S.sarathi_kv8_plan_create(kv, mb, ws.data_ptr(), wsz, cur())
+    q = torch.randn((3, 4096 * 64), device="cuda", generator=g).to(torch.bfloat16)
+    out = torch.full_like(q, float("nan"))
+    S.sarathi_kv8_attention(plan, 0, q.data_ptr(), 4096 * 64, out.data_ptr(), 4096 * 64, cur())
+    worst = float(out.float().abs().max())
+    assert worst <= 2.6e-4 + 4.9e-4 + 0.19 / n ** 0.5
