@@ -151,16 +151,16 @@ int sarathi_kv8_append(const sarathi_kv8_plan* plan, int layer, const void* qkv,
  * must have been appended (its own included):
  *   out[r][h] = sum_j softmax_j(softmax_scale * q[r][h] . k_j) v_j.
  * Scores, softmax and sums in fp32; products on the matrix cores from the
- * codes, which are exact in bf16: bf16 rows multiply as they are, with the
- * probabilities (times the value scale) rounded to bf16; fp32 rows and their
- * probabilities go in as three bf16 terms each (24 bits).  Decodes of bf16 rows
- * over int8 codes multiply in f16 instead: q by a power of two per head (its
- * elements keep their 8 bits down to 2^-28 of the head's largest; a head with a
- * magnitude beyond 2^111 gives NaN), the probabilities (times the value scale)
- * with 11 bits, and dropped below 2^-32 of the largest; sums take the codes as
- * code + 128, so their fp32 roundings are relative to 128 scales, not to the
- * values; the 128 is taken out every 512 keys of a sum, which bounds these
- * roundings by 2^-10 of a code, whatever the number of keys.
+ * codes, which are exact in bf16 and f16.  Chunks of bf16 rows multiply as they
+ * are, with the probabilities (times the value scale) rounded to bf16; fp32 rows
+ * and their probabilities go in as three bf16 terms each (24 bits).  Decodes of
+ * bf16 rows multiply in f16: q by a power of two per head (its elements keep
+ * their 8 bits down to 2^-28 of the head's largest), the probabilities (times
+ * the value scale) with 11 bits, and dropped below 2^-32 of the largest.  Over
+ * int8 codes a head of q with a magnitude beyond 2^111 gives NaN there, and sums
+ * take the codes as code + 128, so their fp32 roundings are relative to 128
+ * scales, not to the values; the 128 is taken out every 512 keys of a sum, which
+ * bounds these roundings by 2^-10 of a code, whatever the number of keys.
  * out [T, ld_out] must not overlap q.
  * Errors: EINVAL (NULL, layer, alignment, overlap), EHIP.
  */

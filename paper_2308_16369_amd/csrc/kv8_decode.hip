@@ -2,8 +2,8 @@
 //
 // Work item = (decode, a range of its keys), one block per item, key/value
 // head and group of 16 query heads; four waves take steps of 32 keys in turn.
-// A wave multiplies on v_mfma_f32_16x16x32_bf16 straight from registers, the
-// codes converted to bf16 (exact for both formats):
+// A wave multiplies on v_mfma_f32_16x16x32_f16 (bf16 rows) or _bf16 (fp32 rows, in
+// three terms) straight from registers, the codes converted exactly:
 //   S^T = K Q^T: A = 16 keys x 32 dims, B = 32 dims x 16 query heads.  A lane
 //     (c = lane % 16, gq = lane / 16) loads 16 bytes of key c at dims
 //     64 i + 16 gq; the product's order over dims is the same permutation on
@@ -49,11 +49,11 @@ __device__ __forceinline__ void store_out4(const Kv8DecodeArgs& a, int row, int 
   else *reinterpret_cast<floatx4*>(out) = x;
 }
 
-// F16: bf16 rows over int8 codes (kv8_device.h).
+// F16: bf16 rows (kv8_device.h).  OFFSET: of them, int8 codes, which enter as code + 128.
 template <typename T, int D, bool INT8>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_kernel(Kv8DecodeArgs a) {
   constexpr int NT = sizeof(T) == 2 ? 1 : 3;
-  constexpr bool F16 = INT8 && NT == 1;
+  constexpr bool F16 = NT == 1, OFFSET = F16 && INT8;
   constexpr int KI = D / 64;             // 16-byte K loads per key row and lane
   constexpr int DB = D / 16;             // V bytes per key row and lane; tiles of O
   constexpr int VW = DB / 4;             // dwords of them
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
       }
       // a power of two that brings the row's largest magnitude to 2^14 .. 2^15
-      const int ex = f16_exponent(groups_max(top));
+      const int ex = f16_exponent(groups_max(top), OFFSET ? 110 : 127);
       const float f = __builtin_ldexpf(1.f, -ex);
 #pragma unroll
       for (int i = 0; i < 2 * KI; ++i)
@@ -98,26 +98,24 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         for (int e = 0; e < 4; ++e) {
           const uint32_t w = pk_f16(x[i][2 * e] * f, x[i][2 * e + 1] * f);
           qf[i][0][e] = w;
-          sum = sum_f16(w, sum);
+          if constexpr (OFFSET) sum = sum_f16(w, sum);
         }
       c_mul = __builtin_ldexpf(a.scale_log2, ex);
-      c_add = -128.f * groups_sum(sum) * c_mul;
-      c_mul *= 16777216.f;
+      if constexpr (OFFSET) {
+        c_add = -128.f * groups_sum(sum) * c_mul;
+        c_mul *= 16777216.f;
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 2 * KI; ++i) {
         const T* p = q + 64 * (i / 2) + 8 * (i & 1);
-        if constexpr (NT == 1) {
-          qf[i][0] = *reinterpret_cast<const u32x4*>(p);
-        } else {
-          float x[8];
-          Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
-          Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
-          bf16x8_t t[NT];
-          split8<NT>(x, t);
+        float x[8];
+        Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
+        Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
+        bf16x8_t t[NT];
+        split8<NT>(x, t);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) qf[i][n] = __builtin_bit_cast(u32x4, t[n]);
-        }
+        for (int n = 0; n < NT; ++n) qf[i][n] = __builtin_bit_cast(u32x4, t[n]);
       }
     }
   }
@@ -186,7 +184,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           if constexpr (F16) {
-            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8_f16(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]),
+            s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8_f16<INT8>(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]),
                                                           __builtin_bit_cast(f16x8_t, qf[2 * i + u][0]), s[h], 0, 0, 0);
           } else {
             const bf16x8_t kf = codes8_bf16<INT8>(t.k[h][i][2 * u], t.k[h][i][2 * u + 1]);
@@ -197,7 +195,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         }
       const float mul = t.ks[h] * c_mul, add = t.ks[h] * c_add;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) s[h][v] = F16 ? fmaf(s[h][v], mul, add) : s[h][v] * mul;
+      for (int v = 0; v < 4; ++v) s[h][v] = OFFSET ? fmaf(s[h][v], mul, add) : s[h][v] * mul;
     }
     if (k0 + 32 > ke) {
 #pragma unroll
@@ -247,7 +245,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         for (int v = 0; v < 2; ++v) {
           const uint32_t pair = pk_f16(p[2 * v], p[2 * v + 1]);
           w[2 * h + v] = pair;
-          lp = sum_f16(pair, lp);
+          if constexpr (OFFSET) lp = sum_f16(pair, lp);
         }
       }
     } else {
@@ -264,30 +262,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_run);
-      if constexpr (NT == 1) {
-        // the row sum takes the rounded probabilities that multiply V: the
-        // weights add up to one, whatever their rounding
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float vs = t.vs[h] > 0.f ? t.vs[h] : 1.f;      // a zero scale belongs to zero codes
-          float sum = 0.f;
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const uint32_t pair = pk_bf16(p[4 * h + 2 * v] * vs, p[4 * h + 2 * v + 1] * vs);
-            w[2 * h + v] = pair;
-            sum = sum_bf16(pair, sum);
-          }
-          l_run = fmaf(sum, 1.0f / vs, l_run);
-        }
-        pf[0] = __builtin_bit_cast(bf16x8_t, u32x4{w[0], w[1], w[2], w[3]});
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          l_run += p[i];
-          p[i] *= t.vs[i >> 2];
-        }
-        split8<NT>(p, pf);
+      for (int i = 0; i < 8; ++i) {
+        l_run += p[i];
+        p[i] *= t.vs[i >> 2];
       }
+      split8<NT>(p, pf);
     }
 #pragma unroll
     for (int x = 0; x < VW; ++x) {
@@ -313,7 +293,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
     }
   };
 
-  // F16: o and lp take the codes with their offset, whose sum outgrows the result
+  // OFFSET: o and lp take the codes with their offset, whose sum outgrows the result
   // the more keys there are.  Taken out every CENTRE steps, it and the roundings
   // of the sums stay those of that many steps: over 2^20 keys in one item a mean
   // is off by 7e-5 of a code (by 1.3e-3 without), over 2^17 by 2e-4 (4e-4).
@@ -338,19 +318,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
     if (k + 32 * NW < ke) load(t0, k + 32 * NW);
     step(t1, k);
     k += 32 * NW;
-    if constexpr (F16) {
+    if constexpr (OFFSET) {
       if ((k - k_first) % (32 * NW * CENTRE) == 0) centre();
     }
   }
   l_run = groups_sum(l_run);
   if constexpr (F16) {
-    // o = 2^24 (sum of p u) - 128 (sum of p) (of the steps since the last centre()), and to units of 2^m_run (m_run -inf:
-    // the wave had no keys, all zeros)
-    const float bias = 128.f * groups_sum(lp), f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M_run - m_run);
+    // to units of 2^m_run (m_run -inf: the wave had no keys, all zeros).  OFFSET: o =
+    // 2^24 (sum of p u) - 128 (sum of p) (of the steps since the last centre())
+    const float f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M_run - m_run);
+    const float bias = OFFSET ? 128.f * groups_sum(lp) : 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) o[db][v] = fmaf(o[db][v], 16777216.f, -bias) * f;
+      for (int v = 0; v < 4; ++v) o[db][v] = (OFFSET ? fmaf(o[db][v], 16777216.f, -bias) : o[db][v]) * f;
   }
 
   // Merge of the waves.  Lane (c, gq) holds dims (D / 4) gq + DB v + db of head c in o[db][v].

@@ -1,18 +1,19 @@
 // Device helpers of the attention over the 8-bit KV cache.
 //
-// Codes become matrix-core operands without rounding.  bf16 holds every code of
-// both formats.  bf16 rows over int8 codes multiply in f16 instead, whose
-// subnormals make the conversion a byte move: u = code + 128 (one xor per four
-// codes) put into the low byte of a half is u 2^-24.  The offset goes out at the
-// end,
+// Codes become matrix-core operands without rounding.  bf16 and f16 both hold
+// every code of both formats.  Chunks and fp32 rows multiply in bf16; decodes of
+// bf16 rows in f16, whose probabilities keep 11 bits instead of 8.  For int8
+// f16's subnormals also make the conversion a byte move: u = code + 128 (one xor
+// per four codes) put into the low byte of a half is u 2^-24.  The offset goes
+// out at the end,
 //   q . code = 2^24 q . (u 2^-24) - 128 sum(q),
 // and alike for V with the sum of the probabilities.  q is scaled by a power of
 // two into f16's range (its 8 bits fit; elements below 2^-28 of the row's
-// largest lose bits, rows beyond 2^111 become NaN), and the probabilities times
-// their value scale are kept at the top of f16's range by a running maximum of
-// their own, so they keep 11 bits; the row sum, which the value scales have no
-// part in, is taken from the weights themselves where the scales lie so far
-// apart that these products would lose weights.
+// largest lose bits; int8: rows beyond 2^111 become NaN), and the probabilities
+// times their value scale are kept at the top of f16's range by a running
+// maximum of their own, so they keep 11 bits; the row sum, which the value
+// scales have no part in, is taken from the weights themselves where the scales
+// lie so far apart that these products would lose weights.
 #pragma once
 
 #include "kv8.h"
@@ -76,26 +77,44 @@ __device__ __forceinline__ uint32_t pk_f16(float a, float b) {   // nearest even
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
 }
 
-// Four int8 codes as u = code + 128: pairs of halves u 2^-24 of codes 0, 1 and 2, 3.
+// Four codes as pairs of halves (codes 0, 1 and 2, 3): int8 as u 2^-24, u = code + 128; e4m3 as they are.
 __device__ __forceinline__ uint32_t offset_codes(uint32_t w) { return w ^ 0x80808080u; }
+template <bool INT8>
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (INT8) {
+    const uint32_t u = offset_codes(w);
+    lo = __builtin_amdgcn_perm(u, u, 0x0c010c00);
+    hi = __builtin_amdgcn_perm(u, u, 0x0c030c02);
+  } else {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+  }
+}
+template <bool INT8>
 __device__ __forceinline__ f16x8_t codes8_f16(uint32_t a, uint32_t b) {
-  const uint32_t x = offset_codes(a), y = offset_codes(b);
-  return __builtin_bit_cast(f16x8_t, (u32x4{__builtin_amdgcn_perm(x, x, 0x0c010c00), __builtin_amdgcn_perm(x, x, 0x0c030c02),
-                                            __builtin_amdgcn_perm(y, y, 0x0c010c00), __builtin_amdgcn_perm(y, y, 0x0c030c02)}));
+  uint32_t x, y, z, t;
+  codes_f16<INT8>(a, x, y);
+  codes_f16<INT8>(b, z, t);
+  return __builtin_bit_cast(f16x8_t, (u32x4{x, y, z, t}));
 }
 // Byte b of eight keys' dwords as one operand (the keys along its eight elements).
 template <bool INT8, bool F16>
 __device__ __forceinline__ void transpose8(const uint32_t* v, u32x4* y) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    if constexpr (F16) {
+    if constexpr (F16 && INT8) {
       const uint32_t w0 = offset_codes(v[2 * e]), w1 = offset_codes(v[2 * e + 1]);
 #pragma unroll
       for (int b = 0; b < 4; ++b) y[b][e] = __builtin_amdgcn_perm(w1, w0, 0x0c040c00 + 0x00010001 * b);
     } else {
       uint32_t lo0, hi0, lo1, hi1;
-      codes_bf16<INT8>(v[2 * e], lo0, hi0);
-      codes_bf16<INT8>(v[2 * e + 1], lo1, hi1);
+      if constexpr (F16) {
+        codes_f16<INT8>(v[2 * e], lo0, hi0);
+        codes_f16<INT8>(v[2 * e + 1], lo1, hi1);
+      } else {
+        codes_bf16<INT8>(v[2 * e], lo0, hi0);
+        codes_bf16<INT8>(v[2 * e + 1], lo1, hi1);
+      }
       y[0][e] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100);
       y[1][e] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302);
       y[2][e] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100);
@@ -103,9 +122,10 @@ __device__ __forceinline__ void transpose8(const uint32_t* v, u32x4* y) {
     }
   }
 }
-// The power of two that brings a row of largest magnitude `top` to 2^14 .. 2^15, as an exponent.
-__device__ __forceinline__ int f16_exponent(float top) {
-  return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 110) - 14;
+// The power of two that brings a row of largest magnitude `top` to 2^14 .. 2^15, as an exponent (at most 2^`most`,
+// which leaves the factor that takes it out of a score room in fp32).
+__device__ __forceinline__ int f16_exponent(float top, int most) {
+  return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), most) - 14;
 }
 __device__ __forceinline__ float sum_f16(uint32_t pair, float c) {
   return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pair), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, c, false);

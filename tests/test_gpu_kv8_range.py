@@ -1,11 +1,13 @@
 """8-bit KV cache, attention at the ends of its range: value scales far apart and beside zero blocks, very long work
-items."""
+items, and the bits that weights keep."""
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from kv8_harness import Batch, Cache, Spec, check_attention, cur  # noqa: E402
+from kv8_harness import Batch, Cache, Spec, check_attention, cur, f64  # noqa: E402
+from oracle import kv8 as ref  # noqa: E402
 from paper_2308_16369_amd import sarathi as S  # noqa: E402
 from test_gpu_kv8 import attend, gen  # noqa: E402
 
@@ -72,3 +74,38 @@ def test_error_does_not_grow_with_the_keys_of_an_item(n):
     S.sarathi_kv8_attention(plan, 0, q.data_ptr(), 4096 * 64, out.data_ptr(), 4096 * 64, cur())
     worst = float(out.float().abs().max())
     assert worst <= 2.6e-4 + 4.9e-4 + 0.19 / n ** 0.5
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_decode_weights_keep_eleven_bits(fmt):
+    """Two keys of nearly equal weights and opposite values, bf16 rows: the weights' rounding shows.
+
+    A weight is off by at most 2^-11 of itself; beside it 2^-8 of the output for its own rounding, and 2^-18 of
+    sum w |v| for the score (fp32, 64 products), the exponential and, int8, the codes' offset."""
+    spec = Spec(heads=64, kv_heads=64, dim=64, dtype="bf16", fmt=fmt, block=16, slots=1, seq=16)
+    cache = Cache(spec)
+    cache.fill(gen(5))
+    codes, scales = cache.views()
+    v1 = codes[0, 0, 1, :, 1]
+    codes[0, 0, 1, :, 0] = v1 ^ 128 if fmt == "e4m3" else (-v1.view(torch.int8)).view(torch.uint8)
+    scales[0, 0, 0] *= 0.02
+    q = torch.randn((1, 64 * 64), device="cuda", generator=gen(6)).to(spec.tdt)
+    out = f64(attend(cache, Batch(decodes=[(0, 1)]), q)).reshape(64, 64)
+    v = cache.values()[0, 0]
+    for h in range(64):
+        o, a, _ = ref.attend(f64(q).reshape(64, 64)[h], v[0, h, :2], v[1, h, :2], 1 / 8)
+        assert np.all(np.abs(out[h] - o) <= (2.0 ** -11 + 2.0 ** -18) * a + 2.0 ** -8 * np.abs(o))
+
+
+def test_e4m3_decodes_take_the_largest_queries():
+    """Query heads of magnitude up to 2^127 over tiny keys: finite scores, finite outputs."""
+    spec = Spec(heads=4, kv_heads=2, dim=64, dtype="bf16", fmt="e4m3", block=16)
+    cache = Cache(spec)
+    cache.fill(gen(8))
+    cache.views()[1][:, :, 0] *= 2.0 ** -88
+    b = Batch(chunks=[(1, 20, 40)], decodes=[(0, 150), (2, 33)])
+    q = torch.randn((b.T, 4 * 64), device="cuda", generator=gen(9)).clamp(-2, 2)
+    q[-2, 64:128] *= 2.0 ** 126
+    q[-1] *= 2.0 ** 88
+    q = q.to(spec.tdt)
+    check_attention(spec, b, cache.values(), q, attend(cache, b, q))
