@@ -9,8 +9,9 @@
 //   lane % 32, g = lane / 32) holding the scores of packed row ql for keys
 //   8 (v / 4) + 4 g + v % 4 of each 32-key half; V^T comes from transposed LDS
 //   reads.  A scale is constant over 16 keys: the key scale joins the softmax
-//   scale in the exponent, the value scale enters there as its logarithm (the
-//   row sum divides it out again), so neither costs a multiplication per score.
+//   scale in the exponent; of bf16 rows the value scale enters there as its
+//   logarithm (the row sum divides it out again), so neither costs a
+//   multiplication per score.
 // 512 rows over a prefix of 2048 (52 heads): 54 us, 0.59 PFLOP/s; a 4096-token
 // prompt (32 / 8 heads): 179 us, 0.77 PFLOP/s.  A wave's tile takes some 4700
 // cycles, of which the matrix cores are busy 1024: it is bound by the latency of
@@ -262,12 +263,12 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
     bf16x8_t pf[2][NT];
     auto probs = [&](bf16x8_t* f, int i) {
-      const float add = __builtin_amdgcn_logf(vs4[i]) - m_use;   // log2
       float p[8], sum = 0.f;
-#pragma unroll
-      for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][8 * (i & 1) + v], ks4[i], add));
-      split8<NT>(p, f);
       if constexpr (NT == 1) {
+        const float add = __builtin_amdgcn_logf(vs4[i]) - m_use;   // log2
+#pragma unroll
+        for (int v = 0; v < 8; ++v) p[v] = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][8 * (i & 1) + v], ks4[i], add));
+        split8<NT>(p, f);
         // the row sum takes the rounded probabilities that multiply V
         const u32x4 w = __builtin_bit_cast(u32x4, f[0]);
 #pragma unroll
@@ -275,11 +276,19 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
           const uint32_t pair = w[e];
           sum = sum_bf16(pair, sum);
         }
+        l_run = fmaf(sum, __builtin_amdgcn_rcpf(vs4[i]), l_run);
       } else {
+        // the logarithm's roundings (2^-24 of its magnitude) would cost fp32 rows
+        // bits: the value scale multiplies, and the row sum does without it
 #pragma unroll
-        for (int v = 0; v < 8; ++v) sum += p[v];
+        for (int v = 0; v < 8; ++v) {
+          p[v] = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][8 * (i & 1) + v], ks4[i], -m_use));
+          sum += p[v];
+          p[v] *= vs4[i];
+        }
+        split8<NT>(p, f);
+        l_run += sum;
       }
-      l_run = fmaf(sum, __builtin_amdgcn_rcpf(vs4[i]), l_run);
     };
     read_v(vf[0], 0);
     probs(pf[0], 0);

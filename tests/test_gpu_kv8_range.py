@@ -109,3 +109,21 @@ def test_e4m3_decodes_take_the_largest_queries():
     q[-1] *= 2.0 ** 88
     q = q.to(spec.tdt)
     check_attention(spec, b, cache.values(), q, attend(cache, b, q))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_fp32_chunk_weights_keep_their_bits_under_tiny_value_scales(fmt):
+    """fp32 rows, 17 equal weights, two of the values not zero, whose scales differ and are near 2^-93: off by the
+    roundings of two products of three terms and their sum, of the row sum's reciprocal and its product: 9 of 2^-23."""
+    spec = Spec(heads=32, kv_heads=32, dim=64, dtype="f32", fmt=fmt, block=16, slots=1, seq=32)
+    cache = Cache(spec)
+    cache.fill(gen(15))
+    codes, scales = cache.views()
+    kept = codes[0, 0, 1].clone()
+    codes.zero_()
+    codes[0, 0, 1, :, [0, 16]] = kept[:, [0, 16]]
+    scales[0, 0, 1] = (1 + torch.rand((32, 2), device="cuda", generator=gen(16))) * 2.0 ** -93
+    q = torch.zeros((17, 32 * 64), device="cuda")
+    out = f64(attend(cache, Batch(chunks=[(0, 0, 17)]), q)).reshape(17, 32, 64)[16]
+    v = cache.values()[0, 0, 1, :, :17]
+    assert np.all(np.abs(out - v.mean(1)) <= 9 * 2.0 ** -23 * np.abs(v).mean(1))
