@@ -161,6 +161,9 @@ int sarathi_kv8_append(const sarathi_kv8_plan* plan, int layer, const void* qkv,
  * take the codes as code + 128, so their fp32 roundings are relative to 128
  * scales, not to the values; the 128 is taken out every 512 keys of a sum, which
  * bounds these roundings by 2^-10 of a code, whatever the number of keys.
+ * The whole range of the cache's values is attended to: sums do not leave fp32's
+ * range, and every key counts in the row sum whatever its value scale.  Value
+ * scales below 2^-120 of the largest that a row sees count as that (or as zero).
  * out [T, ld_out] must not overlap q.
  * Errors: EINVAL (NULL, layer, alignment, overlap), EHIP.
  */

@@ -190,6 +190,7 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
   for (int ks = 0; ks < D / 16; ++ks) koff[ks] = ql * DCH + swz<D>(2 * ks + g, ql);
 
   float ks4[4], vs4[4];
+  float unit = KV8_UNIT;                 // of the row's sums (kv8_device.h)
   auto compute = [&](int it, int buf) {
     const int k0 = kbeg + (NG * it + grp) * KT;
     if (k0 > last_key || k0 >= kend || idle) {
@@ -237,12 +238,19 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
     const bool full = k0 + KT <= kend && k0 + KT - 1 <= offset + r0 + wave * 32 / group;
     if (!full) {
       const int lim = min(qpos, kend - 1) - k0;
+      // scales of keys that the row does not see stay out of its unit and its sums
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vs4[i] = 16 * i <= lim ? vs4[i] : 0.f;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (kb * 32 + 8 * (v >> 2) + 4 * g + (v & 3) > lim) s[kb][v] = -INFINITY;
     }
+    const bool change = kv8_unit_change(fmaxf(fmaxf(vs4[0], vs4[1]), fmaxf(vs4[2], vs4[3])), unit);
+    // a zero scale belongs to zero codes, so 1 does as well
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vs4[i] = vs4[i] > 0.f ? fmaxf(vs4[i], kv8_unit_floor(unit)) : 1.f;
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -252,15 +260,16 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
       mx = max_nan(mx, t * ks4[i]);
     }
     mx = lanes_max(mx);
-    if (__ballot(mx > m_run + 8.0f)) {
-      const float m_new = fmaxf(m_run, mx);
-      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+    if (__ballot(change || mx > m_run + 8.0f)) {
+      const float m_new = fmaxf(m_run, NT == 1 ? mx : __builtin_ceilf(mx));   // fp32 rows: whole, so that m_use is exact
+      float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      corr = change ? corr * KV8_UNIT_STEP : corr;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) o_acc[db] *= corr;
       l_run *= corr;
       m_run = m_new;
     }
-    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    const float m_use = (m_run == -INFINITY ? 0.f : m_run) - unit;
     bf16x8_t pf[2][NT];
     auto probs = [&](bf16x8_t* f, int i) {
       float p[8], sum = 0.f;
@@ -307,11 +316,11 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
   };
 
   auto step = [&](int it, int buf) {
-    // a zero scale belongs to zero codes, so 1 does as well
+    // a zero key scale belongs to zero codes, so 1 does as well
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       ks4[i] = (ks_next[i] > 0.f ? ks_next[i] : 1.f) * a.scale_log2;
-      vs4[i] = vs_next[i] > 0.f ? vs_next[i] : 1.f;
+      vs4[i] = vs_next[i];                 // as the row sees it: below
     }
     if (it + 1 < n_iter) fetch(it + 1);
     compute(it, buf);                      // (the last tile stages itself again, unread)
@@ -326,6 +335,12 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
     if (it + 1 < n_iter) step(it + 1, 1);
   }
   l_run = lanes_sum(l_run);
+  {
+    const float f = kv8_unit_out(unit, m_run);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) o_acc[db] *= f;
+    l_run *= f;
+  }
   if constexpr (NG == 2) {
     // the second group's result through LDS (the tiles are done with) to the first
     float* red_m = reinterpret_cast<float*>(lds);      // [QB] m, [QB] l, [QB][D + 4] o

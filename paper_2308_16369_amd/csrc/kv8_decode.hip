@@ -127,6 +127,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
   // probabilities (at most 2^15) at the top of f16's range: they keep 11 bits
   // down to 2^-21 of the largest and are dropped below 2^-32.
   float m_run = -INFINITY, M_run = -INFINITY, l_run = 0.f, lp = 0.f;
+  float unit = KV8_UNIT;                 // of the sums of fp32 rows (kv8_device.h)
   floatx4 o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -249,23 +250,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
         }
       }
     } else {
-      if (__ballot(mx > m_run + 8.0f)) {
-        const float m_new = fmaxf(m_run, mx);
-        const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      const bool change = kv8_unit_change(fmaxf(t.vs[0], t.vs[1]), unit);
+      if (__ballot(change || mx > m_run + 8.0f)) {
+        const float m_new = fmaxf(m_run, __builtin_ceilf(mx));   // whole: m_use is exact
+        float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        corr = change ? corr * KV8_UNIT_STEP : corr;
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db] *= corr;
         l_run *= corr;
         m_run = m_new;
       }
       float p[8];
+      const float m_use = m_run - unit;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_run);
+        for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_use);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         l_run += p[i];
-        p[i] *= t.vs[i >> 2];
+        p[i] *= fmaxf(t.vs[i >> 2], kv8_unit_floor(unit));
       }
       split8<NT>(p, pf);
     }
@@ -324,14 +328,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
   }
   l_run = groups_sum(l_run);
   if constexpr (F16) {
-    // to units of 2^m_run (m_run -inf: the wave had no keys, all zeros).  OFFSET: o =
-    // 2^24 (sum of p u) - 128 (sum of p) (of the steps since the last centre())
-    const float f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M_run - m_run);
+    // to units of 2^m_run; or m_run and l_run to those of 2^M_run, where o may leave
+    // fp32's range in the others (m_run -inf: the wave had no keys, all zeros).
+    // OFFSET: o = 2^24 (sum of p u) - 128 (sum of p) (since the last centre())
+    const float up = m_run == -INFINITY ? 0.f : M_run - m_run, f = __builtin_amdgcn_exp2f(fminf(up, 0.f));
     const float bias = OFFSET ? 128.f * groups_sum(lp) : 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int v = 0; v < 4; ++v) o[db][v] = (OFFSET ? fmaf(o[db][v], 16777216.f, -bias) : o[db][v]) * f;
+    l_run *= __builtin_amdgcn_exp2f(fminf(-up, 0.f));
+    m_run = fmaxf(m_run, M_run);
+  } else {
+    const float f = kv8_unit_out(unit, m_run);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] *= f;
+    l_run *= f;
   }
 
   // Merge of the waves.  Lane (c, gq) holds dims (D / 4) gq + DB v + db of head c in o[db][v].

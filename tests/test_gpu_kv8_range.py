@@ -127,3 +127,44 @@ def test_fp32_chunk_weights_keep_their_bits_under_tiny_value_scales(fmt):
     out = f64(attend(cache, Batch(chunks=[(0, 0, 17)]), q)).reshape(17, 32, 64)[16]
     v = cache.values()[0, 0, 1, :, :17]
     assert np.all(np.abs(out - v.mean(1)) <= 9 * 2.0 ** -23 * np.abs(v).mean(1))
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_values_near_the_largest_floats(dtype, fmt):
+    """Values up to 2^125: everywhere in one slot, from the middle on in another, in one early block of a third; and
+    near 2^-93 everywhere in a fourth.  Whole and split rows of chunks and decodes."""
+    spec = Spec(heads=4, kv_heads=2, dim=64, dtype=dtype, fmt=fmt, block=64, seq=3000, slots=8)
+    cache = Cache(spec)
+    cache.fill(gen(31))
+    scales = cache.views()[1]
+    up = 2.0 ** (122 if fmt == "e4m3" else 123)
+    scales[0, 0::4, 1] *= up
+    scales[0, 1::4, 1, :, 20:] *= up
+    scales[0, 2::4, 1, :, 1] *= up
+    scales[0, 3::4, 1] *= 2.0 ** -92
+    b = Batch(chunks=[(1, 2500, 30), (4, 0, 40), (2, 2900, 20), (3, 200, 10)], decodes=[(0, 2998), (5, 1500), (6, 100), (7, 700)])
+    q = torch.randn((b.T, 4 * 64), device="cuda", generator=gen(32)).to(spec.tdt)
+    check_attention(spec, b, cache.values(), q, attend(cache, b, q), scales=cache.host()[1])
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_value_scales_up_and_down_by_steps(dtype, fmt):
+    """Value scales that climb from 2^-96 to 2^116 block by block, fall, or do both in turn, under keys of equal scores
+    (no zero codes: every element of an output is of its largest scale)."""
+    spec = Spec(heads=2, kv_heads=1, dim=128, dtype=dtype, fmt=fmt, block=16, seq=700, slots=3)
+    cache = Cache(spec)
+    cache.fill(gen(33))
+    codes, scales = cache.views()
+    codes[(codes & 127) == 0] = 1 if fmt == "int8" else 0x38
+    codes[:, :, 0] = 0
+    n = scales.shape[-1]
+    climb = torch.tensor([-90 + 212 * i // (n - 1) for i in range(n)], device="cuda")
+    scales[:, :, 1] *= torch.exp2(climb.double()).float()
+    scales[:, 1, 1] = scales[:, 1, 1].flip(-1)
+    scales[:, 2, 1, :, 1::2] = scales[:, 2, 1, :, 1::2].flip(-1)
+    for ends in ([699, 699, 699], [200, 500, 333], [64, 80, 31]):
+        b = Batch(chunks=[(i, e - 20, 20) for i, e in enumerate(ends)])
+        q = torch.randn((b.T, 2 * 128), device="cuda", generator=gen(34)).to(spec.tdt)
+        check_attention(spec, b, cache.values(), q, attend(cache, b, q))
+        b = Batch(decodes=[(i, e) for i, e in enumerate(ends)])
+        check_attention(spec, b, cache.values(), q[:3], attend(cache, b, q[:3]), scales=cache.host()[1])
