@@ -261,15 +261,15 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
     }
     mx = lanes_max(mx);
     if (__ballot(change || mx > m_run + 8.0f)) {
-      const float m_new = fmaxf(m_run, NT == 1 ? mx : __builtin_ceilf(mx));   // fp32 rows: whole, so that m_use is exact
-      float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-      corr = change ? corr * KV8_UNIT_STEP : corr;
+      const float m_new = fmaxf(m_run, mx);
+      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      const float corr_o = change ? corr * KV8_UNIT_STEP : corr;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) o_acc[db] *= corr;
-      l_run *= corr;
+      for (int db = 0; db < D / 32; ++db) o_acc[db] *= corr_o;
+      l_run *= NT == 1 ? corr_o : corr;
       m_run = m_new;
     }
-    const float m_use = (m_run == -INFINITY ? 0.f : m_run) - unit;
+    const float m_use = (m_run == -INFINITY ? 0.f : m_run) - (NT == 1 ? unit : 0.f);
     bf16x8_t pf[2][NT];
     auto probs = [&](bf16x8_t* f, int i) {
       float p[8], sum = 0.f;
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
         for (int v = 0; v < 8; ++v) {
           p[v] = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][8 * (i & 1) + v], ks4[i], -m_use));
           sum += p[v];
-          p[v] *= vs4[i];
+          p[v] *= vs4[i] * kv8_unit_pow2(unit);
         }
         split8<NT>(p, f);
         l_run += sum;
@@ -336,6 +336,7 @@ __global__ __launch_bounds__(256 * NG, sizeof(T) == 2 ? 2 : 1) void kv8_attn_chu
   }
   l_run = lanes_sum(l_run);
   {
+    if constexpr (NT > 1) l_run *= kv8_unit_pow2(unit);
     const float f = kv8_unit_out(unit, m_run);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o_acc[db] *= f;

@@ -252,24 +252,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
     } else {
       const bool change = kv8_unit_change(fmaxf(t.vs[0], t.vs[1]), unit);
       if (__ballot(change || mx > m_run + 8.0f)) {
-        const float m_new = fmaxf(m_run, __builtin_ceilf(mx));   // whole: m_use is exact
-        float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-        corr = change ? corr * KV8_UNIT_STEP : corr;
+        const float m_new = fmaxf(m_run, mx);
+        const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        const float corr_o = change ? corr * KV8_UNIT_STEP : corr;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] *= corr;
+        for (int db = 0; db < DB; ++db) o[db] *= corr_o;
         l_run *= corr;
         m_run = m_new;
       }
       float p[8];
-      const float m_use = m_run - unit;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_use);
+        for (int v = 0; v < 4; ++v) p[4 * h + v] = __builtin_amdgcn_exp2f(s[h][v] - m_run);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         l_run += p[i];
-        p[i] *= fmaxf(t.vs[i >> 2], kv8_unit_floor(unit));
+        p[i] *= fmaxf(t.vs[i >> 2], kv8_unit_floor(unit)) * kv8_unit_pow2(unit);
       }
       split8<NT>(p, pf);
     }
@@ -340,6 +339,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void kv8_attn_rows_ker
     l_run *= __builtin_amdgcn_exp2f(fminf(-up, 0.f));
     m_run = fmaxf(m_run, M_run);
   } else {
+    l_run *= kv8_unit_pow2(unit);
     const float f = kv8_unit_out(unit, m_run);
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] *= f;

@@ -71,12 +71,14 @@ __device__ __forceinline__ void split8(const float* x, bf16x8_t* t) {
   }
 }
 
-// Units of a row's sums.  Weights are held as 2^u of themselves, and so are the sums
-// o and l: u is 24, and -40 from the first tile on with a value scale beyond 2^60.
-// So sums of the largest values (scales below 2^121, codes 2^9, weights 2^8, 2^20
-// keys) stay in fp32's range, and the weights under the smallest scales (2^-100)
-// out of its subnormals.  After the change, scales below 2^-60 count as that:
-// 2^-120 of the largest.
+// Units of a row's sums.  The weights that multiply values are held as 2^u of
+// themselves: u is 24, and -40 from the first tile on with a value scale beyond
+// 2^60.  So sums of the largest values (scales below 2^122, codes 2^9, weights
+// 2^8, 2^20 keys) stay in fp32's range, and the weights under the smallest scales
+// (2^-100) out of its subnormals.  After the change, scales below 2^-60 count as
+// that: 2^-120 of the largest.  bf16 rows take u into the exponent (and the row
+// sum with it); fp32 rows, whose weights its rounding there would show in, into
+// the value scale.
 constexpr float KV8_UNIT = 24.f, KV8_UNIT_LARGE = -40.f;
 constexpr float KV8_UNIT_STEP = 5.421010862427522e-20f;    // 2^-64: what o and l take at the change
 // scale: the largest of a tile.  True: the unit changes before it.
@@ -85,6 +87,7 @@ __device__ __forceinline__ bool kv8_unit_change(float scale, float& u) {
   u = change ? KV8_UNIT_LARGE : u;
   return change;
 }
+__device__ __forceinline__ float kv8_unit_pow2(float u) { return u > 0.f ? 16777216.f : 9.094947017729282e-13f; }
 __device__ __forceinline__ float kv8_unit_floor(float u) { return u > 0.f ? 0.f : 8.673617379884035e-19f; }
 // Out of these units: the factor for o and l, exact; or the row's maximum raised, where o may leave fp32's range:
 // (m, l, o) stands for the same as (m + k, l 2^-k, o 2^-k).

@@ -168,3 +168,27 @@ def test_value_scales_up_and_down_by_steps(dtype, fmt):
         check_attention(spec, b, cache.values(), q, attend(cache, b, q))
         b = Batch(decodes=[(i, e) for i, e in enumerate(ends)])
         check_attention(spec, b, cache.values(), q[:3], attend(cache, b, q[:3]), scales=cache.host()[1])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_fp32_weights_are_as_exact_as_their_scores(fmt):
+    """fp32 rows, two keys of scores 0 and s, |s| <= 1/2, and of values 1 and -1: outputs w0 - w1, off by the weights'
+    errors alone.  The score's two roundings (2^-24 |s| each), the exponent's (2^-25), the exponential's own (2^-23)
+    and the row sum's: below 4 2^-24 of a weight, that is 2^-24 of w0 - w1 (w0 w1 <= 1/4).  Root mean square over the
+    heads, chunk row and decode."""
+    spec = Spec(heads=64, kv_heads=64, dim=64, dtype="f32", fmt=fmt, block=16, slots=2, seq=16)
+    cache = Cache(spec)
+    codes, scales = cache.views()
+    codes.zero_()
+    one, minus = (1, 255) if fmt == "int8" else (0x38, 0xb8)
+    codes[0, :, 0, :, 1, 0] = one
+    codes[0, :, 1, :, 0], codes[0, :, 1, :, 1] = one, minus
+    scales.fill_(1.0)
+    b = Batch(chunks=[(0, 0, 2)], decodes=[(1, 1)])
+    q = torch.zeros((3, 64, 64), device="cuda")
+    q[:, :, 0] = 8 * torch.rand((3, 64), device="cuda", generator=gen(17)) - 4
+    out = f64(attend(cache, b, q.view(3, -1))).reshape(3, 64, 64)
+    s = f64(q)[..., 0] / 8
+    for r in (1, 2):
+        err = out[r] - np.tanh(-s[r] / 2)[:, None]
+        assert np.sqrt(np.mean(err ** 2)) <= 2.0 ** -24, np.sqrt(np.mean(err ** 2)) * 2 ** 24
