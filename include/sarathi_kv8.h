@@ -125,7 +125,9 @@ void sarathi_kv8_plan_free(sarathi_kv8_plan* plan);
  * n_kv_heads key heads, then its value heads.  Every q and k head is
  * normalised (qk_norm; q_gain, k_gain: [head_dim] of dtype, shared by the
  * heads) and rotated by the row's position.  q goes to q_out [T, ld_q], which
- * may be qkv itself (ld_q == ld_qkv) and otherwise must not overlap it; k and
+ * may be qkv itself (ld_q == ld_qkv) and otherwise must not overlap it (here and
+ * below, rows overlap where the memory from the first row's start to the last
+ * one's end does: not even the rows' gaps are shared); k and
  * v go to the cache of `layer` at the row's (slot, position).  Strides are in
  * elements; rows must be 16-byte aligned.  Arithmetic in fp32; q is rounded
  * once to dtype, k and v once to their codes (nearest, ties to even).
@@ -135,10 +137,10 @@ void sarathi_kv8_plan_free(sarathi_kv8_plan* plan);
  * positions (those before the first new one) are rounded to the new scale,
  * exactly (save for the smallest) in e4m3, off by at most half a code in int8.
  * A block whose first position is written starts anew.  Scales below 2^-100
- * are zero, and so are the block's values.  The cache holds finite values: an
- * infinity is stored as the largest code of its sign, NaN as zero, and neither
- * counts for the scale.  Nothing but the new positions, those codes and the
- * blocks' scales is written.
+ * are zero, and so are the block's codes and values.  The cache holds finite
+ * values: an infinity is stored as the largest code of its sign (zero where the
+ * scale is zero), NaN as zero, and neither counts for the scale.  Nothing but
+ * the new positions, those codes and the blocks' scales is written.
  * Errors: EINVAL (NULL, layer, alignment, gains missing, q_out overlapping),
  * EHIP.
  */
@@ -196,6 +198,8 @@ int sarathi_kv8_read(const sarathi_kv8_plan* plan, int layer, int out_dtype, voi
  * workspace: sarathi_kv8_workspace_bytes.  The intermediates that
  * sarathi_kv8_workspace_layout places hold the (last) layer's values after a
  * call (qkv: q normalised and rotated, k and v as projected).
+ * sarathi_profile_begin / _end (sarathi.h) do not see these calls: they record
+ * no stages of the 8-bit layer.
  */
 typedef struct {
   sarathi_layer_weights base;

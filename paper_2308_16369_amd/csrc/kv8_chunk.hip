@@ -12,17 +12,20 @@
 //   scale in the exponent; of bf16 rows the value scale enters there as its
 //   logarithm (the row sum divides it out again), so neither costs a
 //   multiplication per score.
-// 512 rows over a prefix of 2048 (52 heads): 54 us, 0.59 PFLOP/s; a 4096-token
-// prompt (32 / 8 heads): 179 us, 0.77 PFLOP/s.  A wave's tile takes some 4700
-// cycles, of which the matrix cores are busy 1024: it is bound by the latency of
-// its own chain (LDS reads, products, maximum, exponentials, products, barrier).
-// Fragments are therefore read a step ahead of their products and the next
-// tile is converted and stored beside the second products; either alone gains
-// 0 to 1 %, both together 6 % on the first case and 2 % on the second.  Tried
-// and no faster: the next tile's products under this one's exponentials, 32-key
-// tiles with three waves per SIMD, 64 rows per wave (the accumulators then move
-// between register files), and operands straight from global memory (440 us for
-// the prompt).
+// Probabilities of bf16 rows are rounded to bf16 (with q and the codes exact, all
+// that the products lose): outputs are off by 2.2e-3 of their magnitude, of which
+// their own rounding is 1.7e-3.
+// 512 rows over a prefix of 2048 (52 heads): 51 us, 0.62 PFLOP/s; a 4096-token
+// prompt (32 / 8 heads) with three decodes: 181 us, 0.76 PFLOP/s.  The matrix
+// cores are busy 21 and 32 % of the cycles: it is bound by the latency of a tile's
+// chain (LDS reads, products, maximum, exponentials, products, barrier) and the
+// vector instructions beside it (10 to 11 per matrix instruction).  Fragments are
+// therefore read a step ahead of their products and the next tile is converted
+// and stored beside the second products; either alone gained 0 to 1 %, both
+// together 6 % on the first case and 2 % on the second.  Tried and no faster: the
+// next tile's products under this one's exponentials, 32-key tiles with three
+// waves per SIMD, 64 rows per wave (the accumulators then move between register
+// files), and operands straight from global memory (440 us for the prompt).
 #include "kv8_device.h"
 
 namespace sarathi {

@@ -18,9 +18,9 @@
 // multiplies the scores with the softmax scale, the value scale the
 // probabilities.
 //
-// 48 decodes of 512 to 2048 tokens (40 heads, int8): 105 us, 6.4 TB/s of codes
+// 48 decodes of 512 to 2048 tokens (40 heads, int8): 104 us, 6.4 TB/s of codes
 // (a plain non-temporal read: 7.1).  Two contexts of 98 and 131 thousand tokens
-// (64 / 8 heads, e4m3): 67 us and 4.6 of the join.  With every code converted to
+// (64 / 8 heads, e4m3): 67 us and 4.6 of the join.  With int8 codes converted to
 // bf16, and rows in batch order, the first took 124 us: the conversions then
 // outlasted the loads.  Nothing is staged in LDS, as no code is used by two waves.
 #include "kv8_device.h"

@@ -47,9 +47,11 @@ struct sarathi_kv8_plan {
 
 namespace {
 
-// Keys of a decode's work item at least (two steps of each of a block's four
-// waves), and the blocks that the decodes of a batch are split into where their
-// keys allow it (three per CU, what runs at once).
+// Keys up to which a decode is one work item whatever the batch (two steps of
+// each of a block's four waves), and the blocks that the decodes of a batch are
+// split into where their keys allow it (three per CU, what runs at once).  Items
+// are whole steps of all four waves, so a row's last item has what is left: of
+// 1025 keys in items of 256, one key.
 constexpr int DEC_MIN_KEYS = 256, DEC_STEP = 128;
 constexpr long DEC_BLOCKS = 768;
 // Chunk attention: key tiles of an item at least, the items that splitting adds
@@ -196,8 +198,8 @@ void plan_chunks(const sarathi_kv8_cfg& c, const BatchDesc& b, HostPlan* p) {
   // choice that ends first: the longest range or the rounds of average ones,
   // with a block's set-up and output, and the combine pass where rows are split.
   // Two groups finish a block in about half the time without splitting its rows:
-  // 512 rows over 2048 keys of 52 heads (208 blocks) take 54 us, one group with
-  // rows split in two 64; three prompts of 347 to 910 rows of 32 / 8 heads 48
+  // 512 rows over 2048 keys of 52 heads (208 blocks) took 54 us, one group with
+  // rows split in two 64, when both were measured; three prompts of 347 to 910 rows of 32 / 8 heads 48
   // against 61; a 4096-token prompt of 32 / 8 heads (1024 blocks), which fills
   // the GPU either way, 189 against 179 of one group.
   int tau = longest;
