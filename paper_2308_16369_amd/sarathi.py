@@ -312,9 +312,16 @@ def sarathi_hybrid_layer_forward_noalloc(cfg, weights: sarathi_layer_weights, kv
     return _check(rc) if check else rc
 
 
+def _layer_array(kind, weights, cfg):
+    """The weights' array of a model step, of which the library reads n_layers entries."""
+    if len(weights) < cfg.n_layers:
+        raise SarathiError(EINVAL, f"weights of {len(weights)} layers, the model has {cfg.n_layers}")
+    return (kind * len(weights))(*weights)
+
+
 def sarathi_model_step(cfg, weights: Sequence[sarathi_layer_weights], kv: KV, batch, x_in: int, x_out: int,
                        ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
-    arr = (sarathi_layer_weights * len(weights))(*weights)
+    arr = _layer_array(sarathi_layer_weights, weights, cfg)
     rc = lib().sarathi_model_step(ct.byref(cfg), arr, kv.handle, ct.byref(batch), ct.c_void_p(x_in),
                                   ct.c_void_p(x_out), ct.c_void_p(ws), ws_bytes, ct.c_void_p(stream))
     return _check(rc) if check else rc
@@ -352,7 +359,7 @@ def sarathi_mixed_layer_forward(cfg, weights: sarathi_layer_weights, kv: KV, lay
 
 def sarathi_mixed_model_step(cfg, weights: Sequence[sarathi_layer_weights], kv: KV, batch, x_in: int, x_out: int,
                              ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
-    arr = (sarathi_layer_weights * len(weights))(*weights)
+    arr = _layer_array(sarathi_layer_weights, weights, cfg)
     rc = lib().sarathi_mixed_model_step(ct.byref(cfg), arr, kv.handle, ct.byref(batch), ct.c_void_p(x_in),
                                         ct.c_void_p(x_out), ct.c_void_p(ws), ws_bytes, ct.c_void_p(stream))
     return _check(rc) if check else rc
@@ -545,9 +552,7 @@ def sarathi_kv8_layer_forward(cfg, weights: sarathi_kv8_layer_weights, kv: KV8, 
 
 def sarathi_kv8_model_step(cfg, weights: Sequence[sarathi_kv8_layer_weights], kv: KV8, batch, x_in: int, x_out: int,
                            ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
-    if len(weights) < cfg.n_layers:      # the library reads n_layers entries
-        raise SarathiError(EINVAL, f"weights of {len(weights)} layers, the model has {cfg.n_layers}")
-    arr = (sarathi_kv8_layer_weights * len(weights))(*weights)
+    arr = _layer_array(sarathi_kv8_layer_weights, weights, cfg)
     rc = lib().sarathi_kv8_model_step(ct.byref(cfg), arr, kv.handle, ct.byref(batch), x_in, x_out, ws, ws_bytes, stream)
     return _check(rc) if check else rc
 
