@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsarathi.so")
 SOURCES = ["runtime.cpp", "scheduler.cpp", "elementwise.hip", "gemm.hip", "chunk_attention.hip", "decode_attention.hip",
-           "attention_combine.hip", "noalloc.hip", "kv8_runtime.cpp", "kv8_append.hip", "kv8_decode.hip", "kv8_chunk.hip"]
+           "attention_combine.hip", "noalloc.hip", "kv8_runtime.cpp", "kv8_append.hip", "kv8_decode.hip", "kv8_chunk.hip",
+           "mx_runtime.cpp", "mx_quantize.hip", "mx_linear.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -1,5 +1,5 @@
-"""ctypes binding of libsarathi.so (see include/sarathi.h, sarathi_sched.h and
-sarathi_kv8.h for the contract).
+"""ctypes binding of libsarathi.so (see include/sarathi.h, sarathi_sched.h,
+sarathi_kv8.h and sarathi_mx.h for the contract).
 
 Argument marshalling only: every step of the layer runs in the library's HIP
 kernels.  The names mirror the C entry points.  Device memory is passed as
@@ -26,6 +26,7 @@ NORM_RMS, NORM_LAYER = 0, 1
 ACT_SWIGLU, ACT_GELU = 0, 1
 LINEAR_PLAIN, LINEAR_RESID, LINEAR_RESID_F32IN, LINEAR_SWIGLU, LINEAR_GELU = 0, 1, 2, 3, 4
 KV8_INT8, KV8_E4M3 = 0, 1
+MX_E2M1, MX_E4M3 = 0, 1
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS = 0, 1, 2, 3
 POLICY_DECODE_MAXIMAL, POLICY_PREFILL_DECODE, POLICY_MIXED = 0, 1, 2
@@ -89,6 +90,11 @@ class sarathi_kv8_cfg(ct.Structure):
 
 class sarathi_kv8_layer_weights(ct.Structure):
     _fields_ = [("base", sarathi_layer_weights), ("q_gain", ct.c_void_p), ("k_gain", ct.c_void_p)]
+
+
+class sarathi_mx_layout(ct.Structure):
+    _fields_ = [(n, ct.c_size_t) for n in ("tile", "unit", "row", "scale_tile", "scale_cols", "scale_half", "scale_row",
+                                           "scale_offset", "total")]
 
 
 class sarathi_kv8_layout(ct.Structure):
@@ -161,6 +167,18 @@ EXPORTS = {
     "sarathi_linear_tiled": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_void_p, ct.c_void_p,
                                         ct.c_void_p, ct.c_void_p, ct.c_void_p, ct.c_size_t, ct.c_int, ct.c_int,
                                         ct.c_void_p]),
+    "sarathi_mx_bytes": (ct.c_size_t, [ct.c_int, ct.c_int, ct.c_int]),
+    "sarathi_mx_get_layout": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.POINTER(sarathi_mx_layout)]),
+    "sarathi_mx_quantize": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_void_p, ct.c_size_t, ct.c_void_p,
+                                       ct.c_size_t, ct.c_void_p]),
+    "sarathi_mx_dequantize": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_void_p, ct.c_size_t, ct.c_int, ct.c_void_p,
+                                         ct.c_size_t, ct.c_void_p]),
+    "sarathi_mx_norm": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_float, ct.c_void_p,
+                                   ct.c_size_t, ct.c_void_p, ct.c_size_t, ct.c_void_p, ct.c_void_p, ct.c_size_t,
+                                   ct.c_void_p, ct.c_size_t, ct.c_void_p]),
+    "sarathi_mx_linear_scratch_bytes": (ct.c_size_t, [ct.c_int, ct.c_int]),
+    "sarathi_mx_linear": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_void_p,
+                                     ct.c_void_p, ct.c_void_p, ct.c_void_p, ct.c_void_p, ct.c_size_t, ct.c_void_p]),
     "sarathi_kv8_bytes": (ct.c_size_t, [ct.POINTER(sarathi_kv8_cfg), ct.c_int, ct.c_int]),
     "sarathi_kv8_alloc": (ct.c_int, [ct.POINTER(sarathi_kv8_cfg), ct.c_int, ct.c_int, ct.c_void_p, ct.c_size_t,
                                      ct.POINTER(ct.c_void_p)]),
@@ -554,6 +572,49 @@ def sarathi_kv8_model_step(cfg, weights: Sequence[sarathi_kv8_layer_weights], kv
                            ws: int, ws_bytes: int, stream: int = 0, check: bool = True) -> int:
     arr = _layer_array(sarathi_kv8_layer_weights, weights, cfg)
     rc = lib().sarathi_kv8_model_step(ct.byref(cfg), arr, kv.handle, ct.byref(batch), x_in, x_out, ws, ws_bytes, stream)
+    return _check(rc) if check else rc
+
+
+# ---------------------------------------------------------------------------- microscaled operands
+
+def sarathi_mx_bytes(format: int, rows: int, cols: int) -> int:
+    return lib().sarathi_mx_bytes(format, rows, cols)
+
+
+def sarathi_mx_get_layout(format: int, rows: int, cols: int) -> sarathi_mx_layout:
+    out = sarathi_mx_layout()
+    _check(lib().sarathi_mx_get_layout(format, rows, cols, ct.byref(out)))
+    return out
+
+
+def sarathi_mx_quantize(dtype: int, format: int, rows: int, cols: int, x: int, ld_x: int, operand: int,
+                        operand_bytes: int, stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_mx_quantize(dtype, format, rows, cols, x, ld_x, operand, operand_bytes, stream)
+    return _check(rc) if check else rc
+
+
+def sarathi_mx_dequantize(format: int, rows: int, cols: int, operand: int, operand_bytes: int, out_dtype: int, out: int,
+                          ld_out: int, stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_mx_dequantize(format, rows, cols, operand, operand_bytes, out_dtype, out, ld_out, stream)
+    return _check(rc) if check else rc
+
+
+def sarathi_mx_norm(stream_dtype: int, dtype: int, format: int, rows: int, cols: int, eps: float, x: int, ld_x: int,
+                    delta: int, ld_delta: int, gain: int, h_out: int, ld_h: int, operand: int, operand_bytes: int,
+                    stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_mx_norm(stream_dtype, dtype, format, rows, cols, eps, x, ld_x, delta or None, ld_delta, gain,
+                               h_out or None, ld_h, operand, operand_bytes, stream)
+    return _check(rc) if check else rc
+
+
+def sarathi_mx_linear_scratch_bytes(M: int, N: int) -> int:
+    return lib().sarathi_mx_linear_scratch_bytes(M, N)
+
+
+def sarathi_mx_linear(dtype: int, kind: int, a_format: int, M: int, N: int, K: int, a: int, w: int, resid: int, out: int,
+                      scratch: int = 0, scratch_bytes: int = 0, stream: int = 0, check: bool = True) -> int:
+    rc = lib().sarathi_mx_linear(dtype, kind, a_format, M, N, K, a, w, resid or None, out, scratch or None,
+                                 scratch_bytes, stream)
     return _check(rc) if check else rc
 
 
