@@ -108,7 +108,12 @@ __device__ __forceinline__ void dma16(const void* src, uint4* dst) {
   __builtin_amdgcn_global_load_lds(src, (lds_void_t*)dst, 16, 0, 0);
 }
 
-// The same with the non-temporal hint (data read once: it does not allocate in
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void dma4(const void* src, uint4* dst) {
+  __builtin_amdgcn_global_load_lds(src, (lds_void_t*)dst, 4, 0, 0);
+}
+
+// dma16 with the non-temporal hint (data read once: it does not allocate in
 // the memory-side cache).
 __device__ __forceinline__ void dma16_stream(const void* src, uint4* dst) {
   __builtin_amdgcn_global_load_lds(src, (lds_void_t*)dst, 16, 0, 2);

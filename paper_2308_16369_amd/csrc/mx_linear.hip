@@ -1,4 +1,7 @@
 // Products of microscaled operands with the epilogues of the linear ops.
+#include <algorithm>
+#include <cmath>
+
 #include "common.h"
 #include "mx.h"
 #include "sarathi_mx.h"
@@ -42,143 +45,527 @@ __device__ __forceinline__ floatx16 mx_mfma(const u32x4& w, uint32_t ws, const u
   }
 }
 
-// Columns n .. n + 3 of row m: v = the sums (SwiGLU: the gate's, up those of the up rows).
-__device__ __forceinline__ void mx_store4(const MxLinearArgs& p, int m, int n, const float* v, const float* up) {
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {   // nearest even; low half = a
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
+}
+
+// silu(z) u with the hardware's reciprocal (a last place of fp32 off, where a division takes ten instructions)
+__device__ __forceinline__ float swiglu_f(float z, float u) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)) * u; }
+
+// Columns n .. n + 3 of row m of the output: v with the residual added, rounded to the output's type.
+__device__ __forceinline__ void mx_store4(const MxLinearArgs& p, int m, int n, float4 v) {
   if (m >= p.M || n >= p.N) return;
   const size_t at = (size_t)m * p.N + n;
   const bool f32_out = p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID;
   const bool f32_res = p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN;
   const bool resid = p.kind == SARATHI_LINEAR_RESID || p.kind == SARATHI_LINEAR_RESID_F32IN;
-  float y[4];
-  const int have = min(4, p.N - n);
-  if (have == 4 && p.N % 4 == 0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = v[i];
+  if (p.N % 4 == 0) {
     if (resid) {
-      float r[4];
       if (f32_res) {
-        const float4 t = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.resid) + at);
-        r[0] = t.x; r[1] = t.y; r[2] = t.z; r[3] = t.w;
+        const float4 r = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.resid) + at);
+        v = make_float4(v.x + r.x, v.y + r.y, v.z + r.z, v.w + r.w);
       } else {
-        const uint2 t = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p.resid) + at);
-        r[0] = __uint_as_float(t.x << 16); r[1] = __uint_as_float(t.x & 0xffff0000u);
-        r[2] = __uint_as_float(t.y << 16); r[3] = __uint_as_float(t.y & 0xffff0000u);
+        const uint2 r = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p.resid) + at);
+        v = make_float4(v.x + __uint_as_float(r.x << 16), v.y + __uint_as_float(r.x & 0xffff0000u),
+                        v.z + __uint_as_float(r.y << 16), v.w + __uint_as_float(r.y & 0xffff0000u));
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] += r[i];
-    } else if (p.kind == SARATHI_LINEAR_SWIGLU) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = silu_f(y[i]) * up[i];
-    } else if (p.kind == SARATHI_LINEAR_GELU) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = gelu_f(y[i]);
     }
-    if (f32_out) {
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
-    } else {
+    if (f32_out)
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = v;
+    else
       *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(p.out) + at) =
-          make_uint2((uint32_t)f2bf(y[0]) | ((uint32_t)f2bf(y[1]) << 16), (uint32_t)f2bf(y[2]) | ((uint32_t)f2bf(y[3]) << 16));
-    }
+          make_uint2(pk_bf16(v.x, v.y), pk_bf16(v.z, v.w));
     return;
   }
-  for (int i = 0; i < have; ++i) {
-    float z = v[i];
+  const float y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (n + i >= p.N) break;
+    float z = y[i];
     if (resid)
       z += f32_res ? reinterpret_cast<const float*>(p.resid)[at + i] : bf2f(reinterpret_cast<const bf16*>(p.resid)[at + i]);
-    else if (p.kind == SARATHI_LINEAR_SWIGLU) z = silu_f(z) * up[i];
-    else if (p.kind == SARATHI_LINEAR_GELU) z = gelu_f(z);
     if (f32_out) reinterpret_cast<float*>(p.out)[at + i] = z;
     else reinterpret_cast<bf16*>(p.out)[at + i] = f2bf(z);
   }
 }
 
-// A block's waves take 64 W rows (SwiGLU: 32 of the gate and their 32 of up) and 32 rows of x, each wave its share of
-// the columns; the first wave adds the others' sums in order.
-template <int FMT, bool EXACT>
-__global__ __launch_bounds__(256) void mx_linear_kernel(MxLinearArgs p, int tiles_m) {
-  constexpr int XU = FMT == E2M1 ? 1 : 2;             // 16-byte units of a lane per 64 columns
-  __shared__ float join[3][2 * 16 * 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
-  const int n_tiles = (p.N + 31) / 32;
+// W tile t of a product's columns (SwiGLU: even ones are tiles of the gate, odd ones those of up): bytes from the first
+// one's codes and scales.
+__device__ __forceinline__ int w_tile(const MxLinearArgs& p, int t, size_t& up) {
+  const int last = (p.N + 31) / 32 - 1;
   const bool glu = p.kind == SARATHI_LINEAR_SWIGLU;
-  const u32x4* w[2];
-  const uint32_t* ws[2];
+  up = glu && (t & 1) ? p.up : 0;
+  return min(glu ? t >> 1 : t, last);
+}
+
+template <int I, int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+
+// ============================================================================ few rows
+// The weights stream once, from memory into registers, as fragments: FN W tiles to a block (SwiGLU: a gate tile and its up
+// tile), all FM tiles of x (L2 holds them), NW waves each with every NW-th quad of columns, requested one quad ahead.  The
+// waves' sums are joined through LDS in a fixed order, the upper half of the waves first.
+template <int FMT, bool EXACT, int NW, int FN, int FM>
+__global__ __launch_bounds__(64 * NW) void mx_stream_kernel(MxLinearArgs p) {
+  constexpr int XU = FMT == E2M1 ? 1 : 2;             // 16-byte units of a lane per 64 columns
+  constexpr int TILES = FN * FM;
+  __shared__ float4 join[NW / 2 * TILES * 4 * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const u32x4* w[FN];
+  const uint32_t* ws[FN];
 #pragma unroll
-  for (int f = 0; f < 2; ++f) {
-    const int t = min(glu ? tn : 2 * tn + f, n_tiles - 1);
-    const size_t up = glu && f ? p.up : 0;
+  for (int f = 0; f < FN; ++f) {
+    size_t up;
+    const int t = w_tile(p, FN * blockIdx.x + f, up);
     w[f] = reinterpret_cast<const u32x4*>(p.w + up) + (size_t)t * p.quads * 256 + lane;
     ws[f] = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p.w_scale) + up) + (size_t)t * p.quads * 64 + lane;
   }
-  const int row = min(lane & 31, p.M - 1 - tm * 32);   // rows past the last: the last one's
-  const u32x4* x = reinterpret_cast<const u32x4*>(p.a) + (size_t)tm * p.quads * 256 * XU + (lane & 32) + row;
-  const uint32_t* xs = p.a_scale + (size_t)tm * p.quads * 64 + (lane & 32) + row;
-  floatx16 acc[2];
+  const u32x4* x[FM];
+  const uint32_t* xs[FM];
 #pragma unroll
-  for (int f = 0; f < 2; ++f)
+  for (int f = 0; f < FM; ++f) {
+    const int at = (lane & 32) + min(lane & 31, p.M - 1 - f * 32);   // rows past the last: the last one's
+    x[f] = reinterpret_cast<const u32x4*>(p.a) + (size_t)f * p.quads * 256 * XU + at;
+    xs[f] = p.a_scale + (size_t)f * p.quads * 64 + at;
+  }
+  floatx16 acc[FN][FM];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[f][i] = 0.f;
-  for (int q = wave; q < p.quads; q += 4) {
-    u32x4 wf[2][4], xf[4][XU];
-    uint32_t wsc[2];
+  for (int f = 0; f < FN; ++f)
 #pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      wsc[f] = ws[f][(size_t)q * 64];
+    for (int g = 0; g < FM; ++g)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) wf[f][k] = w[f][(size_t)q * 256 + k * 64];
-    }
-    const uint32_t xsc = xs[(size_t)q * 64];
+      for (int i = 0; i < 16; ++i) acc[f][g][i] = 0.f;
+
+  u32x4 wf[4][FN], xf[4][FM][XU];
+  uint32_t wsc[2][FN], xsc[2][FM];
+  auto load = [&](int q, int k) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int f = 0; f < FN; ++f) wf[k][f] = w[f][(size_t)q * 256 + k * 64];
 #pragma unroll
-      for (int u = 0; u < XU; ++u) xf[k][u] = x[((size_t)q * 4 + k) * 64 * XU + u * 64];
+    for (int f = 0; f < FM; ++f)
 #pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      acc[f] = mx_mfma<FMT, EXACT, 0>(wf[f][0], wsc[f], xf[0], xsc, acc[f]);
-      acc[f] = mx_mfma<FMT, EXACT, 1>(wf[f][1], wsc[f], xf[1], xsc, acc[f]);
-      acc[f] = mx_mfma<FMT, EXACT, 2>(wf[f][2], wsc[f], xf[2], xsc, acc[f]);
-      acc[f] = mx_mfma<FMT, EXACT, 3>(wf[f][3], wsc[f], xf[3], xsc, acc[f]);
+      for (int u = 0; u < XU; ++u) xf[k][f][u] = x[f][((size_t)q * 4 + k) * 64 * XU + u * 64];
+  };
+  auto load_scales = [&](int q, int b) {
+#pragma unroll
+    for (int f = 0; f < FN; ++f) wsc[b][f] = ws[f][(size_t)q * 64];
+#pragma unroll
+    for (int f = 0; f < FM; ++f) xsc[b][f] = xs[f][(size_t)q * 64];
+  };
+  if (wave < p.quads) {
+    load_scales(wave, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) load(wave, k);
+    for (int q = wave; q < p.quads; q += NW) {
+      const int next = min(q + NW, p.quads - 1);      // past the last: read again, not used
+      load_scales(next, 1);
+      static_for<0, 4>([&](auto kc) {
+        constexpr int K = decltype(kc)::value;
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+          for (int g = 0; g < FM; ++g)
+            acc[f][g] = mx_mfma<FMT, EXACT, K>(wf[K][f], wsc[0][f], xf[K][g], xsc[0][g], acc[f][g]);
+        load(next, K);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+#pragma unroll
+      for (int f = 0; f < FN; ++f) wsc[0][f] = wsc[1][f];
+#pragma unroll
+      for (int f = 0; f < FM; ++f) xsc[0][f] = xsc[1][f];
     }
   }
-  if (wave) {
+
+  // join[wave of a half][tile, group of four][lane]
+  auto put = [&](int at) {
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int f = 0; f < FN; ++f)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) join[wave - 1][(f * 16 + i) * 64 + lane] = acc[f][i];
+      for (int g = 0; g < FM; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          join[((at * TILES + f * FM + g) * 4 + i) * 64 + lane] =
+              make_float4(acc[f][g][4 * i], acc[f][g][4 * i + 1], acc[f][g][4 * i + 2], acc[f][g][4 * i + 3]);
+  };
+  if (wave >= NW / 2) put(wave - NW / 2);
+  __syncthreads();
+  if (wave < NW / 2) {
+#pragma unroll
+    for (int f = 0; f < FN; ++f)
+#pragma unroll
+      for (int g = 0; g < FM; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 t = join[((wave * TILES + f * FM + g) * 4 + i) * 64 + lane];
+          acc[f][g][4 * i] += t.x; acc[f][g][4 * i + 1] += t.y; acc[f][g][4 * i + 2] += t.z; acc[f][g][4 * i + 3] += t.w;
+        }
+    put(wave);                                        // where it has just read
   }
   __syncthreads();
-  if (wave) return;
+  const bool glu = p.kind == SARATHI_LINEAR_SWIGLU;
+  auto sum = [&](int part) {
+    float4 v = join[part * 64 + lane];
 #pragma unroll
-  for (int f = 0; f < 2; ++f)
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      acc[f][i] = ((acc[f][i] + join[0][(f * 16 + i) * 64 + lane]) + join[1][(f * 16 + i) * 64 + lane]) +
-                  join[2][(f * 16 + i) * 64 + lane];
-  const int m = tm * 32 + (lane & 31);
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int n = (glu ? tn * 32 : tn * 64) + 8 * g + 4 * (lane >> 5);
-    float v[2][4];
-#pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[f][i] = acc[f][4 * g + i];
-    mx_store4(p, m, n, v[0], v[1]);
-    if (!glu) mx_store4(p, m, n + 32, v[1], v[1]);
+    for (int h = 1; h < NW / 2; ++h) {
+      const float4 t = join[(h * TILES * 4 + part) * 64 + lane];
+      v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
+    }
+    return v;
+  };
+  for (int part = wave; part < (glu ? FM * 4 : TILES * 4); part += NW) {   // 32 rows of x by eight W rows
+    const int f = part / (FM * 4), g = part / 4 % FM, i = part % 4;
+    float4 v = sum(part);
+    if (glu) {
+      const float4 u = sum(FM * 4 + part);
+      v = make_float4(swiglu_f(v.x, u.x), swiglu_f(v.y, u.y), swiglu_f(v.z, u.z), swiglu_f(v.w, u.w));
+    } else if (p.kind == SARATHI_LINEAR_GELU) {
+      v = make_float4(gelu_f(v.x), gelu_f(v.y), gelu_f(v.z), gelu_f(v.w));
+    }
+    const int tile = glu ? (int)blockIdx.x : FN * (int)blockIdx.x + f;
+    mx_store4(p, g * 32 + (lane & 31), tile * 32 + 8 * i + 4 * (lane >> 5), v);
   }
+}
+
+// ============================================================================ many rows
+// WGN x WGM waves of FN W tiles by FM tiles of x; a block per CU runs its tiles one after the other.  A stage holds 64
+// columns of a tile's operands, copied to LDS by DMA as they lie in memory: 1 KB per tile of e2m1, 2 of e4m3, lane after
+// lane as the instruction takes them, so reads are free of bank conflicts.  NS stages in a ring.  A wave multiplies stage
+// s while it reads stage s + 1 from LDS.  Before the products of stage s:
+//   wait for stage s + 1 (and the reads of stage s, which the stage before ended with), barrier;
+// then every wave has read stage s, so its place takes stage s + NS: requests run NS - 1 stages ahead, across the tiles
+// of the block, so a tile starts with its operands there, and its output leaves while the next one's arrive.  Requests
+// past the last stage re-read it into places that nothing reads.  The scales, a dword per lane, tile and 256 columns, go
+// the same way (the compiler drains the DMA for any other load in the loop): requested four such quads ahead, before the
+// stage's own requests, and read from LDS with the quad's first fragments.
+//
+// SwiGLU: W tiles come in pairs, gate and up.  With FN = 2 a wave has both of a pair; with FN = 1 it takes 16 rows of each
+// as one fragment, so that either way a lane holds both sums of an output element.
+template <int OFF>
+__device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {   // the compiler would wait for the DMA it may overlap
+  u32x4 v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_read4(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ds_read_b32 %0, %1" : "=v"(v) : "v"(addr));
+  return v;
+}
+template <typename V, int N>
+__device__ __forceinline__ void pin_regs(V (&r)[N]) {      // no use of r moves above this point
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(r[i]));
+}
+constexpr int MX_MAX_STAGES = 12;
+template <int FMT, int WGN, int WGM, int FN, int FM>
+struct MxTile {
+  static constexpr int XU = FMT == E2M1 ? 1 : 2;
+  static constexpr int TN = WGN * FN, TM = WGM * FM, NW = WGN * WGM;
+  static constexpr int STAGE = (TN + TM * XU) * 1024;                         // bytes
+  static constexpr int SCALES = (TN + TM) * 256, SR = 4;                     // of a quad; quads in the ring
+  static constexpr int UNITS = STAGE / 1024, PER = (UNITS + NW - 1) / NW;    // 1 KB requests of a stage, of a wave
+  static constexpr int SPER = (TN + TM + NW - 1) / NW;                       // requests of a quad's scales, of a wave
+  static constexpr int PAD = 36;                                             // floats of a row of the epilogue's tile
+  static constexpr int OUT = NW * 32 * PAD * 4;
+  static constexpr int most(int a, int b) { return a < b ? a : b; }
+  static constexpr int NS = most(most((160 * 1024 - SR * SCALES - OUT) / STAGE, (56 - 3 * SPER) / PER), MX_MAX_STAGES);
+  static constexpr int LDS = SR * SCALES + NS * STAGE + OUT;
+  // requests of scales in the last n steps before step j of a quad (one at each step 0, before the stage's own)
+  static constexpr int scale_requests(int j, int n) { return n >= j ? (n - j) / 4 + (j > 0) : 0; }
+};
+
+template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
+__global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs p, int tiles_m, int tiles_n) {
+  using T = MxTile<FMT, WGN, WGM, FN, FM>;
+  constexpr int XU = T::XU, TN = T::TN, TM = T::TM, NW = T::NW, NS = T::NS, STAGE = T::STAGE;
+  constexpr int UNITS = T::UNITS, PER = T::PER, SPER = T::SPER, SR = T::SR;
+  constexpr int NR = FN + FM * XU, NM = FN * FM;                             // LDS reads and products of a stage
+  static_assert(NS >= 3 && NS <= 4 * SR, "ring");
+  extern __shared__ uint4 lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = wave % WGN, wm = wave / WGN;
+
+  // XCD-aware order: block b runs on XCD b % 8, each XCD takes consecutive tiles, its blocks in turn; eight x tiles by one
+  // panel of W, then the next panel, so that what runs at once shares both
+  const int n_tiles = tiles_m * tiles_n, per = (n_tiles + 7) / 8, stride = gridDim.x / 8;
+  const int t_first = (blockIdx.x % 8) * per + blockIdx.x / 8, t_end = min((int)(blockIdx.x % 8 + 1) * per, n_tiles);
+  if (t_first >= t_end) return;
+  auto place = [&](int t, int& tm, int& tn) {
+    constexpr int GM = 8;
+    const int group = t / (GM * tiles_n), in = t % (GM * tiles_n), gm = min(GM, tiles_m - group * GM);
+    tm = group * GM + in % gm;
+    tn = in / gm;
+  };
+
+  // requests: unit j * NW + wave of a stage: W tiles, then x tiles (e4m3: two units)
+  const int nst = p.quads * 4;
+  const char* src[PER];
+  int r_tile = t_first, r_stage = 0, r_slot = 0;
+  auto aim = [&](int t) {                            // the requests' tile
+    int tm, tn;
+    place(t, tm, tn);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = min(j * NW + wave, UNITS - 1);
+      if (i < TN) {
+        size_t up;
+        const int wt = w_tile(p, tn * TN + i, up);
+        src[j] = p.w + up + (size_t)wt * p.quads * 4096;
+      } else {
+        const int xt = min(tm * TM + (i - TN) / XU, (p.M + 31) / 32 - 1);
+        src[j] = p.a + (size_t)xt * p.quads * 4096 * XU + ((i - TN) % XU) * 1024;
+      }
+    }
+  };
+  auto request = [&](int j) {
+    const int u = min(j * NW + wave, UNITS - 1);
+    dma16(src[j] + lane * 16, lds + (SR * T::SCALES + r_slot * STAGE + u * 1024) / 16);
+    src[j] += u < TN ? 1024 : 1024 * XU;
+  };
+  auto requested = [&]() {                           // a stage: on to the next, or the next tile's first
+    r_slot = r_slot + 1 == NS ? 0 : r_slot + 1;
+    if (++r_stage == nst) {
+      r_stage = 0;
+      if (r_tile + stride < t_end) r_tile += stride;
+      aim(r_tile);
+    }
+  };
+  const char* ssrc[SPER];
+  int s_tile = t_first, s_quad = 0, s_slot = 0;
+  auto aim_scales = [&](int t) {
+    int tm, tn;
+    place(t, tm, tn);
+#pragma unroll
+    for (int j = 0; j < SPER; ++j) {
+      const int u = min(j * NW + wave, TN + TM - 1);
+      size_t up = 0;
+      const int i = u < TN ? w_tile(p, tn * TN + u, up) : min(tm * TM + u - TN, (p.M + 31) / 32 - 1);
+      ssrc[j] = reinterpret_cast<const char*>(u < TN ? p.w_scale : p.a_scale) + up + (size_t)i * p.quads * 256;
+    }
+  };
+  auto request_scales = [&]() {
+#pragma unroll
+    for (int j = 0; j < SPER; ++j) {
+      dma4(ssrc[j] + lane * 4, lds + (s_slot * T::SCALES + min(j * NW + wave, TN + TM - 1) * 256) / 16);
+      ssrc[j] += 256;
+    }
+    s_slot = (s_slot + 1) % SR;
+    if (++s_quad == p.quads) {
+      s_quad = 0;
+      if (s_tile + stride < t_end) s_tile += stride;
+      aim_scales(s_tile);
+    }
+  };
+
+  floatx16 acc[FN][FM];
+  const bool glu = p.kind == SARATHI_LINEAR_SWIGLU;
+  // this lane's place in the W tiles, in fragments of a tile (16 bytes of codes, 4 of scales), and in the x tiles
+  const int wplace = FN == 1 && glu ? ((wn & ~1) + (lane >> 4 & 1)) * 64 + (lane & 32) + (lane & 15) + 16 * (wn & 1)
+                                    : wn * FN * 64 + lane;
+  const int xplace = (TN + wm * FM * XU) * 64 + lane, xsplace = (TN + wm * FM) * 64 + lane;
+  const uint32_t s0 = (uint32_t)(uintptr_t)lds, l0 = s0 + SR * T::SCALES;
+  const uint32_t wl = l0 + wplace * 16, xl = l0 + xplace * 16;
+  u32x4 fr[2][NR];                                   // fragments of a stage: W, then x
+  auto read = [&](auto buf, uint32_t at, auto r) {   // fragment r of the stage at `at`
+    constexpr int B = decltype(buf)::value, R = decltype(r)::value;
+    if constexpr (R < FN) fr[B][R] = lds_read16<R * 1024>(wl + at);
+    else fr[B][R] = lds_read16<(R - FN) * 1024>(xl + at);
+  };
+  uint32_t sc[FN + FM], sc_next[FN + FM];            // the quad's scales: W, then x
+  int sc_slot = 0;
+  auto read_scales = [&](uint32_t* d) {
+    const uint32_t b = s0 + sc_slot * T::SCALES;
+#pragma unroll
+    for (int f = 0; f < FN + FM; ++f) d[f] = lds_read4(b + (f < FN ? wplace + f * 64 : xsplace + (f - FN) * 64) * 4);
+    sc_slot = (sc_slot + 1) % SR;
+  };
+  using C0 = std::integral_constant<int, 0>;
+  using C1 = std::integral_constant<int, 1>;
+  auto landed = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+
+  aim(t_first);
+  aim_scales(t_first);
+  static_for<0, 4 * SR>([&](auto t) {                // steps -4 SR .. -1: at step s, stage s + NS; at 4 q, scales of quad q + SR
+    constexpr int S = decltype(t)::value - 4 * SR;
+    if constexpr (S % 4 == 0) request_scales();
+    if constexpr (S >= -NS) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) request(j);
+      requested();
+    }
+  });
+  wait_vmcnt<(NS - 1) * PER + (NS - 1) / 4 * SPER>();   // quad 0's scales and stage 0
+  lds_barrier();
+  read_scales(sc);
+  static_for<0, NR>([&](auto r) { read(C0{}, 0, r); });
+  landed();
+  pin_regs(sc);
+  pin_regs(fr[0]);
+
+  int slot = 0;
+  auto stage = [&](auto jc) {                        // J of a quad's four
+    constexpr int J = decltype(jc)::value, B = J & 1;
+    const int next = slot + 1 == NS ? 0 : slot + 1;
+    // stage s + 1: younger are the requests of NS - 2 stages, with those of a quad's scales before some
+    wait_vmcnt<(NS - 2) * PER + T::scale_requests(J, NS - 2) * SPER>();
+    lds_barrier();
+    if constexpr (J == 0) request_scales();
+    static_for<0, NM>([&](auto i) {
+      constexpr int I = decltype(i)::value, fm = I / FN, fn = I % FN;
+      acc[fn][fm] = mx_mfma<FMT, EXACT, J>(fr[B][fn], sc[fn], &fr[B][FN + fm * XU], sc[FN + fm], acc[fn][fm]);
+      // the next stage's reads in the first three quarters of the products, requests beside all of them
+      constexpr int SPREAD = (NM * 3 + 3) / 4, R0 = I * NR / SPREAD, R1 = (I + 1) * NR / SPREAD;
+      static_for<(R0 < NR ? R0 : NR), (R1 < NR ? R1 : NR)>(
+          [&](auto r) { read(std::integral_constant<int, 1 - B>{}, next * STAGE, r); });
+      static_for<I * PER / NM, (I + 1) * PER / NM>([&](auto j) { request(decltype(j)::value); });
+      if constexpr (J == 3 && I == 0) read_scales(sc_next);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    requested();
+    slot = next;
+    landed();
+    pin_regs(fr[1 - B]);
+    if constexpr (J == 3) {
+      pin_regs(sc_next);
+#pragma unroll
+      for (int f = 0; f < FN + FM; ++f) sc[f] = sc_next[f];
+    }
+  };
+
+  float* out = reinterpret_cast<float*>(lds + (SR * T::SCALES + NS * STAGE) / 16) + wave * (32 * T::PAD);
+  for (int t = t_first; t < t_end; t += stride) {
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int j = 0; j < FM; ++j)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+    for (int q = 0; q < p.quads; ++q) static_for<0, 4>([&](auto j) { stage(j); });
+
+    // The output, 32 rows by W (16 or 32) columns at a time through the wave's part of LDS, so that it leaves in larger
+    // pieces of its rows.
+    int tm, tn;
+    place(t, tm, tn);
+    auto leave = [&](auto width, auto count, auto&& value) {   // value(f, fm, k): element k of the wave's output tile f
+      constexpr int W = decltype(width)::value, FO = decltype(count)::value, PR = 256 / W;   // rows that leave at once
+      static_for<0, FM * FO>([&](auto ic) {
+        constexpr int I = decltype(ic)::value, fm = I / FO, f = I % FO;
+#pragma unroll
+        for (int g = 0; g < W / 8; ++g)
+          *reinterpret_cast<float4*>(out + (lane & 31) * T::PAD + 8 * g + 4 * (lane >> 5)) =
+              make_float4(value(f, fm, 4 * g), value(f, fm, 4 * g + 1), value(f, fm, 4 * g + 2), value(f, fm, 4 * g + 3));
+        const int r = lane / (W / 4), c = lane % (W / 4) * 4;
+        const int m = (tm * TM + wm * FM + fm) * 32 + r, n = ((tn * WGN + wn) * FO + f) * W + c;
+#pragma unroll
+        for (int i = 0; i < 32; i += PR)
+          mx_store4(p, m + i, n, *reinterpret_cast<const float4*>(out + (r + i) * T::PAD + c));
+      });
+    };
+    using W32 = std::integral_constant<int, 32>;
+    if (glu) {
+      if constexpr (FN == 1)
+        leave(std::integral_constant<int, 16>{}, C1{},
+              [&](int, int fm, int k) { return swiglu_f(acc[0][fm][k], acc[0][fm][k + 8]); });
+      else
+        leave(W32{}, std::integral_constant<int, FN / 2>{},
+              [&](int f, int fm, int k) { return swiglu_f(acc[2 * f][fm][k], acc[2 * f + 1][fm][k]); });
+    } else if (p.kind == SARATHI_LINEAR_GELU) {
+      leave(W32{}, std::integral_constant<int, FN>{}, [&](int f, int fm, int k) { return gelu_f(acc[f][fm][k]); });
+    } else {
+      leave(W32{}, std::integral_constant<int, FN>{}, [&](int f, int fm, int k) { return acc[f][fm][k]; });
+    }
+  }
+  wait_vmcnt<0>();                                   // requests past the last tile still fill the stages
 }
 
 size_t mx_linear_parts(int, int) { return 0; }
 
-hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s) {
-  const int tiles_m = mx_tiles(a.M), cols = a.kind == SARATHI_LINEAR_SWIGLU ? 32 : 64;
-  const dim3 grid(tiles_m * ((a.N + cols - 1) / cols));
-  const bool f32_out = a.dtype == SARATHI_F32 || a.kind == SARATHI_LINEAR_RESID;
-  if (a_format == E2M1) hipLaunchKernelGGL((mx_linear_kernel<E2M1, false>), grid, dim3(256), 0, s, a, tiles_m);
-  else if (f32_out) hipLaunchKernelGGL((mx_linear_kernel<E4M3, true>), grid, dim3(256), 0, s, a, tiles_m);
-  else hipLaunchKernelGGL((mx_linear_kernel<E4M3, false>), grid, dim3(256), 0, s, a, tiles_m);
+template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
+static hipError_t run_tile(const MxLinearArgs& a, hipStream_t s) {
+  using T = MxTile<FMT, WGN, WGM, FN, FM>;
+  const auto kernel = mx_tile_kernel<FMT, EXACT, WGN, WGM, FN, FM>;
+  static std::atomic<uint64_t> lds_set{0};           // devices on which this instance's LDS limit is raised
+  hipError_t e = ensure_dynamic_lds((const void*)kernel, T::LDS, lds_set);
+  if (e != hipSuccess) return e;
+  const int w_tiles = (a.kind == SARATHI_LINEAR_SWIGLU ? 2 : 1) * mx_tiles(a.N);
+  const int tiles_n = (w_tiles + T::TN - 1) / T::TN, tiles_m = (mx_tiles(a.M) + T::TM - 1) / T::TM;
+  const int grid = std::min((tiles_n * tiles_m + 7) / 8 * 8, 256);   // a block per CU
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * T::NW), T::LDS, s, a, tiles_m, tiles_n);
   return hipGetLastError();
+}
+
+template <int FMT, bool EXACT, int NW, int FN, int FM>
+static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s) {
+  const int w_tiles = (a.kind == SARATHI_LINEAR_SWIGLU ? 2 : 1) * mx_tiles(a.N);
+  hipLaunchKernelGGL((mx_stream_kernel<FMT, EXACT, NW, FN, FM>), dim3((w_tiles + FN - 1) / FN), dim3(64 * NW), 0, s, a);
+  return hipGetLastError();
+}
+
+// The tiles of the second kernel, and what 64 columns of one cost on a CU: a fixed part (barrier, waits) and one per
+// product of a W tile and an x tile, in units of 0.14 us (fitted to one round of 80 stages, 2048 to 4096 products per
+// column of the output: e2m1 rows 16.6, 17.8, 24.6, 29.4, 31.4, 37.0 us in the order below, e4m3 18.9, 21.8, 30.6, 38.4,
+// 41.2, 52.9).  A launch takes whole rounds of one tile per CU.  Exact products cost twice the matrix instructions and the
+// split of every x fragment, which FN W tiles share.
+struct TileCost {
+  int tn, tm;
+  float exact;
+};
+constexpr TileCost kTiles[] = {{4, 2, 0.21f}, {4, 4, 0.18f}, {8, 4, 0.145f}, {4, 10, 0.20f}, {8, 6, 0.143f}, {8, 8, 0.118f}};
+
+static int pick_tile(int w_tiles, int x_tiles, int format, bool exact) {
+  int best = 0;
+  float least = INFINITY;
+  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+    const TileCost& t = kTiles[i];
+    const long tiles = (long)((w_tiles + t.tn - 1) / t.tn) * ((x_tiles + t.tm - 1) / t.tm);
+    const float cost = (float)((tiles + 255) / 256) *
+                       (1.0f + t.tn * t.tm * (exact ? t.exact : format == E2M1 ? 0.037f : 0.057f));
+    if (cost < least) least = cost, best = i;
+  }
+  return best;
+}
+
+template <int FMT, bool EXACT>
+static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s) {
+  const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
+  const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
+  // Up to 64 rows stream; up to 128 where the W tiles leave CUs idle in the other kernel (128 rows of 5120 x 13824: 29
+  // us, 35 there; of 15360 x 5120 27 and 23).
+  if (x_tiles <= 2 || (x_tiles <= 4 && w_tiles <= 256)) {
+    switch (x_tiles) {
+      case 1:
+        if (glu) return run_stream<FMT, EXACT, 8, 2, 1>(a, s);
+        return w_tiles <= 256 ? run_stream<FMT, EXACT, 16, 1, 1>(a, s) : run_stream<FMT, EXACT, 8, 1, 1>(a, s);
+      case 2:
+        if (glu) return run_stream<FMT, EXACT, 8, 2, 2>(a, s);
+        if constexpr (FMT == E2M1)                    // (e4m3: the registers of 16 waves do not hold a quad)
+          if (w_tiles <= 256) return run_stream<FMT, EXACT, 16, 1, 2>(a, s);
+        return run_stream<FMT, EXACT, 8, 1, 2>(a, s);
+      case 3: return glu ? run_stream<FMT, EXACT, 4, 2, 3>(a, s) : run_stream<FMT, EXACT, 8, 1, 3>(a, s);
+      default: return glu ? run_stream<FMT, EXACT, 4, 2, 4>(a, s) : run_stream<FMT, EXACT, 4, 1, 4>(a, s);
+    }
+  }
+  switch (pick_tile(w_tiles, x_tiles, FMT, EXACT)) {
+    case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, s);
+    case 1: return run_tile<FMT, EXACT, 4, 2, 1, 2>(a, s);
+    case 2: return run_tile<FMT, EXACT, 4, 2, 2, 2>(a, s);
+    case 3: return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, s);
+    case 4: return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, s);
+    default: return run_tile<FMT, EXACT, 2, 4, 4, 2>(a, s);
+  }
+}
+
+hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s) {
+  const bool f32_out = a.dtype == SARATHI_F32 || a.kind == SARATHI_LINEAR_RESID;
+  if (a_format == E2M1) return linear_as<E2M1, false>(a, s);
+  return f32_out ? linear_as<E4M3, true>(a, s) : linear_as<E4M3, false>(a, s);
 }
 
 }  // namespace sarathi
