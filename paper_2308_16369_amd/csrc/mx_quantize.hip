@@ -8,6 +8,8 @@
 // Eight elements to a lane, four lanes to a block; the largest magnitude is
 // taken over the bit patterns, which puts infinities and NaN above every
 // number.
+#include <type_traits>
+
 #include "common.h"
 #include "mx.h"
 #include "sarathi_mx.h"
@@ -178,13 +180,26 @@ hipError_t launch_mx_dequantize(int dtype, int format, const MxQuantArgs& a, hip
 
 // ------------------------------------------------------------------ norm
 // One row per block, read once and kept in registers (eight elements to a lane,
-// NC times).  The mean and the product are in fp64: an element is then rounded
-// once to fp32 and once to its code, which fp32 products would now and then put
-// on the other side of a code's border.
+// NC times).  An element is rounded once to fp32 and once to its code: squares
+// are added in fp64, and h r g is made of h g with its remainder and of r in two
+// parts.  (Plain fp32 products, two roundings more, would now and then put it on
+// the other side of a code's border.)
 //
 // A row's output is 16-byte pieces 512 bytes apart, so the 32 rows of a tile
 // run on one XCD, one after the other, and their pieces meet in its L2 before
 // they leave it as whole lines.
+template <typename T> struct Raw8 {   // eight elements as they lie in memory
+  uint4 u[8 / Vec16<T>::N];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < 8 / Vec16<T>::N; ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void unpack(float* v) const {
+#pragma unroll
+    for (int i = 0; i < 8 / Vec16<T>::N; ++i) Vec16<T>::unpack(u[i], v + i * Vec16<T>::N);
+  }
+};
+
 template <typename TS, typename T, int FMT, int NC>
 __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, size_t scale_offset) {
   __shared__ double red[4];
@@ -193,22 +208,34 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
   if (row >= (size_t)a.rows) return;
   const TS* x = reinterpret_cast<const TS*>(a.x) + row * a.ld_x;
   const T* d = reinterpret_cast<const T*>(a.delta) + row * a.ld_delta;
-  float v[NC][8], g[NC][8];
+  float v[NC][8];
+  Raw8<TS> xr[NC];
+  Raw8<T> dr[NC], g[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int col = (threadIdx.x + 256 * j) * 8;
+    if (col >= a.cols) continue;
+    xr[j].load(x + col);
+    if (a.delta) dr[j].load(d + col);
+  }
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int col = (threadIdx.x + 256 * j) * 8;
+    if (col < a.cols) g[j].load(reinterpret_cast<const T*>(a.gain) + col);
+  }
   double ss = 0;
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
     const int col = (threadIdx.x + 256 * j) * 8;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][e] = g[j][e] = 0.f;
     if (col >= a.cols) continue;
-    load8(x + col, v[j]);
-    load8(reinterpret_cast<const T*>(a.gain) + col, g[j]);
+    xr[j].unpack(v[j]);
     if (a.delta) {
       float t[8];
-      load8(d + col, t);
+      dr[j].unpack(t);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[j][e] += t[e];
     }
+    if (a.h) store8(reinterpret_cast<TS*>(a.h) + row * a.ld_h + col, v[j]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += (double)v[j][e] * (double)v[j][e];
   }
@@ -217,20 +244,26 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
   __syncthreads();
   const double rs = 1.0 / sqrt((red[0] + red[1] + red[2] + red[3]) / a.cols + (double)a.eps);
+  int k;                                            // r = (rh + rl) 2^k: h 2^k is of the row's own scale
+  const double m = frexp(rs, &k);
+  const float rh = (float)m, rl = (float)(m - (double)rh);
   char* codes = a.operand + (size_t)tile * quads * (32 * (FMT == E2M1 ? 128 : 256));
   uint32_t* scales = reinterpret_cast<uint32_t*>(a.operand + scale_offset) + (size_t)tile * quads * 64;
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
     const int c = threadIdx.x + 256 * j;
     if (c >= quads * 32) continue;                  // whole groups of 32 lanes
-    if (a.h && c * 8 < a.cols) store8(reinterpret_cast<TS*>(a.h) + row * a.ld_h + c * 8, v[j]);
+    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // padding, also in a row of NaN
+    if (c * 8 < a.cols) {
+      float t[8];
+      g[j].unpack(t);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][e] = (float)((double)v[j][e] * rs * (double)g[j][e]);
-    if (c * 8 >= a.cols) {                          // padding, also in a row of NaN
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
+      for (int e = 0; e < 8; ++e) {
+        const float h = ldexpf(v[j][e], k), p = h * t[e];
+        y[e] = __builtin_fmaf(p, rh, __builtin_fmaf(p, rl, __builtin_fmaf(h, t[e], -p) * rh));
+      }
     }
-    put8<FMT>(codes, scales, r, c, v[j], true);
+    put8<FMT>(codes, scales, r, c, y, true);
   }
 }
 
@@ -239,10 +272,16 @@ static hipError_t norm_as(const MxNormArgs& a, hipStream_t s) {
   const int quads = mx_quads(a.cols), nc = (quads * 32 + 255) / 256;
   const size_t at = mx_scale_offset(FMT, a.rows, a.cols);
   const dim3 grid((mx_tiles(a.rows) + 7) / 8 * 256);
-  if (nc <= 1) hipLaunchKernelGGL((mx_norm_kernel<TS, T, FMT, 1>), grid, dim3(256), 0, s, a, quads, at);
-  else if (nc <= 3) hipLaunchKernelGGL((mx_norm_kernel<TS, T, FMT, 3>), grid, dim3(256), 0, s, a, quads, at);
-  else if (nc <= 6) hipLaunchKernelGGL((mx_norm_kernel<TS, T, FMT, 6>), grid, dim3(256), 0, s, a, quads, at);
-  else hipLaunchKernelGGL((mx_norm_kernel<TS, T, FMT, 12>), grid, dim3(256), 0, s, a, quads, at);
+  auto run = [&](auto n) {
+    hipLaunchKernelGGL((mx_norm_kernel<TS, T, FMT, decltype(n)::value>), grid, dim3(256), 0, s, a, quads, at);
+  };
+  if (nc <= 1) run(std::integral_constant<int, 1>{});
+  else if (nc <= 2) run(std::integral_constant<int, 2>{});
+  else if (nc <= 3) run(std::integral_constant<int, 3>{});
+  else if (nc <= 4) run(std::integral_constant<int, 4>{});
+  else if (nc <= 6) run(std::integral_constant<int, 6>{});
+  else if (nc <= 8) run(std::integral_constant<int, 8>{});
+  else run(std::integral_constant<int, 12>{});
   return hipGetLastError();
 }
 template <typename TS, typename T>
