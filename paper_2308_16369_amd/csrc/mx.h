@@ -54,7 +54,7 @@ struct MxLinearArgs {
   size_t up;               // SwiGLU: bytes from gate to up, codes and scales alike
   const void* resid;
   void* out;
-  float* parts;            // or NULL
+  float* parts;            // [split][M][N], or NULL
   size_t parts_cap;        // floats
 };
 hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s);

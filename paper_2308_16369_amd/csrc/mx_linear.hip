@@ -282,7 +282,7 @@ struct MxTile {
 };
 
 template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
-__global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs p, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs p, int tiles_m, int tiles_n, int splits) {
   using T = MxTile<FMT, WGN, WGM, FN, FM>;
   constexpr int XU = T::XU, TN = T::TN, TM = T::TM, NW = T::NW, NS = T::NS, STAGE = T::STAGE;
   constexpr int UNITS = T::UNITS, PER = T::PER, SPER = T::SPER, SR = T::SR;
@@ -294,33 +294,41 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
 
   // XCD-aware order: block b runs on XCD b % 8, each XCD takes consecutive tiles, its blocks in turn; eight x tiles by one
   // panel of W, then the next panel, so that what runs at once shares both
-  const int n_tiles = tiles_m * tiles_n, per = (n_tiles + 7) / 8, stride = gridDim.x / 8;
+  const int n_tiles = tiles_m * tiles_n * splits, per = (n_tiles + 7) / 8, stride = gridDim.x / 8;
   const int t_first = (blockIdx.x % 8) * per + blockIdx.x / 8, t_end = min((int)(blockIdx.x % 8 + 1) * per, n_tiles);
   if (t_first >= t_end) return;
-  auto place = [&](int t, int& tm, int& tn) {
+  struct Place {
+    int tm, tn, split, q0, quads;                    // the tile, its share of the columns
+  };
+  auto place = [&](int t) {
     constexpr int GM = 8;
+    Place a;
+    a.split = t / (tiles_m * tiles_n);
+    t -= a.split * (tiles_m * tiles_n);
     const int group = t / (GM * tiles_n), in = t % (GM * tiles_n), gm = min(GM, tiles_m - group * GM);
-    tm = group * GM + in % gm;
-    tn = in / gm;
+    a.tm = group * GM + in % gm;
+    a.tn = in / gm;
+    a.q0 = (int)((long)p.quads * a.split / splits);
+    a.quads = (int)((long)p.quads * (a.split + 1) / splits) - a.q0;
+    return a;
   };
 
   // requests: unit j * NW + wave of a stage: W tiles, then x tiles (e4m3: two units)
-  const int nst = p.quads * 4;
   const char* src[PER];
-  int r_tile = t_first, r_stage = 0, r_slot = 0;
+  int r_tile = t_first, r_left = 0, r_slot = 0;
   auto aim = [&](int t) {                            // the requests' tile
-    int tm, tn;
-    place(t, tm, tn);
+    const Place a = place(t);
+    r_left = a.quads * 4;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int i = min(j * NW + wave, UNITS - 1);
       if (i < TN) {
         size_t up;
-        const int wt = w_tile(p, tn * TN + i, up);
-        src[j] = p.w + up + (size_t)wt * p.quads * 4096;
+        const int wt = w_tile(p, a.tn * TN + i, up);
+        src[j] = p.w + up + ((size_t)wt * p.quads + a.q0) * 4096;
       } else {
-        const int xt = min(tm * TM + (i - TN) / XU, (p.M + 31) / 32 - 1);
-        src[j] = p.a + (size_t)xt * p.quads * 4096 * XU + ((i - TN) % XU) * 1024;
+        const int xt = min(a.tm * TM + (i - TN) / XU, (p.M + 31) / 32 - 1);
+        src[j] = p.a + ((size_t)xt * p.quads + a.q0) * 4096 * XU + ((i - TN) % XU) * 1024;
       }
     }
   };
@@ -331,23 +339,22 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
   };
   auto requested = [&]() {                           // a stage: on to the next, or the next tile's first
     r_slot = r_slot + 1 == NS ? 0 : r_slot + 1;
-    if (++r_stage == nst) {
-      r_stage = 0;
+    if (--r_left == 0) {
       if (r_tile + stride < t_end) r_tile += stride;
       aim(r_tile);
     }
   };
   const char* ssrc[SPER];
-  int s_tile = t_first, s_quad = 0, s_slot = 0;
+  int s_tile = t_first, s_left = 0, s_slot = 0;
   auto aim_scales = [&](int t) {
-    int tm, tn;
-    place(t, tm, tn);
+    const Place a = place(t);
+    s_left = a.quads;
 #pragma unroll
     for (int j = 0; j < SPER; ++j) {
       const int u = min(j * NW + wave, TN + TM - 1);
       size_t up = 0;
-      const int i = u < TN ? w_tile(p, tn * TN + u, up) : min(tm * TM + u - TN, (p.M + 31) / 32 - 1);
-      ssrc[j] = reinterpret_cast<const char*>(u < TN ? p.w_scale : p.a_scale) + up + (size_t)i * p.quads * 256;
+      const int i = u < TN ? w_tile(p, a.tn * TN + u, up) : min(a.tm * TM + u - TN, (p.M + 31) / 32 - 1);
+      ssrc[j] = reinterpret_cast<const char*>(u < TN ? p.w_scale : p.a_scale) + up + ((size_t)i * p.quads + a.q0) * 256;
     }
   };
   auto request_scales = [&]() {
@@ -357,8 +364,7 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
       ssrc[j] += 256;
     }
     s_slot = (s_slot + 1) % SR;
-    if (++s_quad == p.quads) {
-      s_quad = 0;
+    if (--s_left == 0) {
       if (s_tile + stride < t_end) s_tile += stride;
       aim_scales(s_tile);
     }
@@ -447,12 +453,11 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
       for (int j = 0; j < FM; ++j)
 #pragma unroll
         for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
-    for (int q = 0; q < p.quads; ++q) static_for<0, 4>([&](auto j) { stage(j); });
+    const Place at = place(t);
+    for (int q = 0; q < at.quads; ++q) static_for<0, 4>([&](auto j) { stage(j); });
 
     // The output, 32 rows by W (16 or 32) columns at a time through the wave's part of LDS, so that it leaves in larger
     // pieces of its rows.
-    int tm, tn;
-    place(t, tm, tn);
     auto leave = [&](auto width, auto count, auto&& value) {   // value(f, fm, k): element k of the wave's output tile f
       constexpr int W = decltype(width)::value, FO = decltype(count)::value, PR = 256 / W;   // rows that leave at once
       static_for<0, FM * FO>([&](auto ic) {
@@ -462,10 +467,13 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
           *reinterpret_cast<float4*>(out + (lane & 31) * T::PAD + 8 * g + 4 * (lane >> 5)) =
               make_float4(value(f, fm, 4 * g), value(f, fm, 4 * g + 1), value(f, fm, 4 * g + 2), value(f, fm, 4 * g + 3));
         const int r = lane / (W / 4), c = lane % (W / 4) * 4;
-        const int m = (tm * TM + wm * FM + fm) * 32 + r, n = ((tn * WGN + wn) * FO + f) * W + c;
+        const int m = (at.tm * TM + wm * FM + fm) * 32 + r, n = ((at.tn * WGN + wn) * FO + f) * W + c;
 #pragma unroll
-        for (int i = 0; i < 32; i += PR)
-          mx_store4(p, m + i, n, *reinterpret_cast<const float4*>(out + (r + i) * T::PAD + c));
+        for (int i = 0; i < 32; i += PR) {
+          const float4 v = *reinterpret_cast<const float4*>(out + (r + i) * T::PAD + c);
+          if (splits == 1) mx_store4(p, m + i, n, v);
+          else if (m + i < p.M && n < p.N) *reinterpret_cast<float4*>(p.parts + ((size_t)at.split * p.M + m + i) * p.N + n) = v;
+        }
       });
     };
     using W32 = std::integral_constant<int, 32>;
@@ -476,7 +484,7 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
       else
         leave(W32{}, std::integral_constant<int, FN / 2>{},
               [&](int f, int fm, int k) { return swiglu_f(acc[2 * f][fm][k], acc[2 * f + 1][fm][k]); });
-    } else if (p.kind == SARATHI_LINEAR_GELU) {
+    } else if (p.kind == SARATHI_LINEAR_GELU && splits == 1) {
       leave(W32{}, std::integral_constant<int, FN>{}, [&](int f, int fm, int k) { return gelu_f(acc[f][fm][k]); });
     } else {
       leave(W32{}, std::integral_constant<int, FN>{}, [&](int f, int fm, int k) { return acc[f][fm][k]; });
@@ -485,10 +493,28 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
   wait_vmcnt<0>();                                   // requests past the last tile still fill the stages
 }
 
-size_t mx_linear_parts(int, int) { return 0; }
+// The partial sums of `splits` shares of the columns, added in order; four columns to a thread.
+__global__ __launch_bounds__(256) void mx_join_kernel(MxLinearArgs p, int splits) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, size = (size_t)p.M * p.N;
+  if (i * 4 >= size) return;
+  float4 v = reinterpret_cast<const float4*>(p.parts)[i];
+  for (int s = 1; s < splits; ++s) {
+    const float4 t = *reinterpret_cast<const float4*>(p.parts + s * size + i * 4);
+    v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
+  }
+  if (p.kind == SARATHI_LINEAR_GELU) v = make_float4(gelu_f(v.x), gelu_f(v.y), gelu_f(v.z), gelu_f(v.w));
+  mx_store4(p, (int)(i * 4 / p.N), (int)(i * 4 % p.N), v);
+}
+
+// Most that split columns can use: at most 256 tiles run, of 64 K output elements at most; eight splits.
+constexpr int MX_MAX_SPLITS = 8;
+size_t mx_linear_parts(int M, int N) {
+  if (M <= 64) return 0;
+  return std::min((size_t)MX_MAX_SPLITS * M * N, (size_t)256 * 65536);
+}
 
 template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
-static hipError_t run_tile(const MxLinearArgs& a, hipStream_t s) {
+static hipError_t run_tile(const MxLinearArgs& a, int splits, hipStream_t s) {
   using T = MxTile<FMT, WGN, WGM, FN, FM>;
   const auto kernel = mx_tile_kernel<FMT, EXACT, WGN, WGM, FN, FM>;
   static std::atomic<uint64_t> lds_set{0};           // devices on which this instance's LDS limit is raised
@@ -496,8 +522,11 @@ static hipError_t run_tile(const MxLinearArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   const int w_tiles = (a.kind == SARATHI_LINEAR_SWIGLU ? 2 : 1) * mx_tiles(a.N);
   const int tiles_n = (w_tiles + T::TN - 1) / T::TN, tiles_m = (mx_tiles(a.M) + T::TM - 1) / T::TM;
-  const int grid = std::min((tiles_n * tiles_m + 7) / 8 * 8, 256);   // a block per CU
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * T::NW), T::LDS, s, a, tiles_m, tiles_n);
+  const int grid = std::min((tiles_n * tiles_m * splits + 7) / 8 * 8, 256);   // a block per CU
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * T::NW), T::LDS, s, a, tiles_m, tiles_n, splits);
+  e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  hipLaunchKernelGGL(mx_join_kernel, dim3((unsigned)(((size_t)a.M * a.N / 4 + 255) / 256)), dim3(256), 0, s, a, splits);
   return hipGetLastError();
 }
 
@@ -509,25 +538,36 @@ static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s) {
 }
 
 // The tiles of the second kernel, and what 64 columns of one cost on a CU: a fixed part (barrier, waits) and one per
-// product of a W tile and an x tile, in units of 0.14 us (fitted to one round of 80 stages, 2048 to 4096 products per
-// column of the output: e2m1 rows 16.6, 17.8, 24.6, 29.4, 31.4, 37.0 us in the order below, e4m3 18.9, 21.8, 30.6, 38.4,
-// 41.2, 52.9).  A launch takes whole rounds of one tile per CU.  Exact products cost twice the matrix instructions and the
-// split of every x fragment, which FN W tiles share.
+// product of a W tile and an x tile, in units of 0.14 us (fitted to one round of 80 stages: e2m1 rows 16.6, 17.8, 24.6,
+// 29.4, 31.4, 37.0 us in the order below, e4m3 18.9, 21.8, 30.6, 38.4, 41.2, 52.9).  A launch takes whole rounds of one
+// tile per CU.  Exact products cost twice the matrix instructions and the split of every x fragment, which FN W tiles
+// share.  Where tiles leave CUs idle, the columns are split: shorter tiles, but the partial sums are written and read
+// back, and a launch of their own joins them (320 rows of 5120 x 13824, e2m1: SPLITFIG).
 struct TileCost {
   int tn, tm;
   float exact;
 };
 constexpr TileCost kTiles[] = {{4, 2, 0.21f}, {4, 4, 0.18f}, {8, 4, 0.145f}, {4, 10, 0.20f}, {8, 6, 0.143f}, {8, 8, 0.118f}};
 
-static int pick_tile(int w_tiles, int x_tiles, int format, bool exact) {
-  int best = 0;
+struct TilePick {
+  int tile, splits;
+};
+static TilePick pick_tile(const MxLinearArgs& a, int w_tiles, int x_tiles, int format, bool exact) {
+  TilePick best{0, 1};
   float least = INFINITY;
+  const size_t size = (size_t)a.M * a.N;
+  // (partial sums of SwiGLU would be two for each output, and its W tiles are many)
+  const bool can_split = a.parts && a.kind != SARATHI_LINEAR_SWIGLU && a.N % 4 == 0;
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const TileCost& t = kTiles[i];
     const long tiles = (long)((w_tiles + t.tn - 1) / t.tn) * ((x_tiles + t.tm - 1) / t.tm);
-    const float cost = (float)((tiles + 255) / 256) *
-                       (1.0f + t.tn * t.tm * (exact ? t.exact : format == E2M1 ? 0.037f : 0.057f));
-    if (cost < least) least = cost, best = i;
+    for (int n = 1; n <= MX_MAX_SPLITS; ++n) {
+      if (n > 1 && (!can_split || n * tiles > 256 || a.quads < 4 * n || n * size > a.parts_cap)) break;
+      const float stages = (float)((tiles * n + 255) / 256) * ((a.quads + n - 1) / n) * 4;
+      float us = 0.14f * stages * (1.0f + t.tn * t.tm * (exact ? t.exact : format == E2M1 ? 0.037f : 0.057f));
+      if (n > 1) us += 4.0f + n * size * 8e-6f / 5.0f;   // the launch; partial sums written and read, 5 TB/s
+      if (us < least) least = us, best = {i, n};
+    }
   }
   return best;
 }
@@ -552,13 +592,14 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s) {
       default: return glu ? run_stream<FMT, EXACT, 4, 2, 4>(a, s) : run_stream<FMT, EXACT, 4, 1, 4>(a, s);
     }
   }
-  switch (pick_tile(w_tiles, x_tiles, FMT, EXACT)) {
-    case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, s);
-    case 1: return run_tile<FMT, EXACT, 4, 2, 1, 2>(a, s);
-    case 2: return run_tile<FMT, EXACT, 4, 2, 2, 2>(a, s);
-    case 3: return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, s);
-    case 4: return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, s);
-    default: return run_tile<FMT, EXACT, 2, 4, 4, 2>(a, s);
+  const TilePick pick = pick_tile(a, w_tiles, x_tiles, FMT, EXACT);
+  switch (pick.tile) {
+    case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, pick.splits, s);
+    case 1: return run_tile<FMT, EXACT, 4, 2, 1, 2>(a, pick.splits, s);
+    case 2: return run_tile<FMT, EXACT, 4, 2, 2, 2>(a, pick.splits, s);
+    case 3: return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, pick.splits, s);
+    case 4: return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, pick.splits, s);
+    default: return run_tile<FMT, EXACT, 2, 4, 4, 2>(a, pick.splits, s);
   }
 }
 
