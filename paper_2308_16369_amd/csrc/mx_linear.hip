@@ -54,41 +54,49 @@ __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {   // nearest eve
 // silu(z) u with the hardware's reciprocal (a last place of fp32 off, where a division takes ten instructions)
 __device__ __forceinline__ float swiglu_f(float z, float u) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)) * u; }
 
-// Columns n .. n + 3 of row m of the output: v with the residual added, rounded to the output's type.
-__device__ __forceinline__ void mx_store4(const MxLinearArgs& p, int m, int n, float4 v) {
-  if (m >= p.M || n >= p.N) return;
+__device__ __forceinline__ bool adds_resid(const MxLinearArgs& p) {
+  return p.kind == SARATHI_LINEAR_RESID || p.kind == SARATHI_LINEAR_RESID_F32IN;
+}
+// The residual at columns n .. n + 3 of row m (N a multiple of 4).
+__device__ __forceinline__ float4 load_resid4(const MxLinearArgs& p, int m, int n) {
   const size_t at = (size_t)m * p.N + n;
-  const bool f32_out = p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID;
-  const bool f32_res = p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN;
-  const bool resid = p.kind == SARATHI_LINEAR_RESID || p.kind == SARATHI_LINEAR_RESID_F32IN;
-  if (p.N % 4 == 0) {
-    if (resid) {
-      if (f32_res) {
-        const float4 r = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.resid) + at);
-        v = make_float4(v.x + r.x, v.y + r.y, v.z + r.z, v.w + r.w);
-      } else {
-        const uint2 r = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p.resid) + at);
-        v = make_float4(v.x + __uint_as_float(r.x << 16), v.y + __uint_as_float(r.x & 0xffff0000u),
-                        v.z + __uint_as_float(r.y << 16), v.w + __uint_as_float(r.y & 0xffff0000u));
-      }
-    }
-    if (f32_out)
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = v;
-    else
-      *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(p.out) + at) =
-          make_uint2(pk_bf16(v.x, v.y), pk_bf16(v.z, v.w));
-    return;
+  if (p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN)
+    return *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.resid) + at);
+  const uint2 r = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p.resid) + at);
+  return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                     __uint_as_float(r.y & 0xffff0000u));
+}
+// Columns n .. n + 3 of row m of the output, rounded to its type (N a multiple of 4).
+__device__ __forceinline__ void put4(const MxLinearArgs& p, int m, int n, const float4& v) {
+  const size_t at = (size_t)m * p.N + n;
+  if (p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID)
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = v;
+  else
+    *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(p.out) + at) = make_uint2(pk_bf16(v.x, v.y), pk_bf16(v.z, v.w));
+}
+// The same for any N, with the residual added.
+__device__ __forceinline__ void put_any(const MxLinearArgs& p, int m, int n, float4 v) {
+#pragma unroll 1
+  for (int i = 0; i < 4 && n + i < p.N; ++i) {
+    const size_t at = (size_t)m * p.N + n + i;
+    float z = v.x;
+    v = make_float4(v.y, v.z, v.w, v.x);
+    if (adds_resid(p))
+      z += p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN
+               ? reinterpret_cast<const float*>(p.resid)[at]
+               : bf2f(reinterpret_cast<const bf16*>(p.resid)[at]);
+    if (p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID) reinterpret_cast<float*>(p.out)[at] = z;
+    else reinterpret_cast<bf16*>(p.out)[at] = f2bf(z);
   }
-  const float y[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (n + i >= p.N) break;
-    float z = y[i];
-    if (resid)
-      z += f32_res ? reinterpret_cast<const float*>(p.resid)[at + i] : bf2f(reinterpret_cast<const bf16*>(p.resid)[at + i]);
-    if (f32_out) reinterpret_cast<float*>(p.out)[at + i] = z;
-    else reinterpret_cast<bf16*>(p.out)[at + i] = f2bf(z);
-  }
+}
+__device__ __forceinline__ float4 add4(const float4& a, const float4& b) {
+  return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
+// One such piece from sums v.
+__device__ __forceinline__ void mx_store4(const MxLinearArgs& p, int m, int n, const float4& v) {
+  if (m >= p.M || n >= p.N) return;
+  if (p.N % 4) put_any(p, m, n, v);
+  else put4(p, m, n, adds_resid(p) ? add4(v, load_resid4(p, m, n)) : v);
 }
 
 // W tile t of a product's columns (SwiGLU: even ones are tiles of the gate, odd ones those of up): bytes from the first
@@ -234,11 +242,11 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(MxLinearArgs p) {
 }
 
 // ============================================================================ many rows
-// WGN x WGM waves of FN W tiles by FM tiles of x; a block per CU runs its tiles one after the other.  A stage holds 64
-// columns of a tile's operands, copied to LDS by DMA as they lie in memory: 1 KB per tile of e2m1, 2 of e4m3, lane after
-// lane as the instruction takes them, so reads are free of bank conflicts.  NS stages in a ring.  A wave multiplies stage
-// s while it reads stage s + 1 from LDS.  Before the products of stage s:
-//   wait for stage s + 1 (and the reads of stage s, which the stage before ended with), barrier;
+// WGN x WGM waves of FN W tiles by FM tiles of x; a block per CU runs its tiles one after the other.  A stage holds CS
+// steps of 64 columns of a tile's operands, copied to LDS by DMA as they lie in memory: 1 KB per tile and step of e2m1, 2
+// of e4m3, lane after lane as the instruction takes them, so reads are free of bank conflicts.  NS stages in a ring.  A
+// wave multiplies a step while it reads the next one from LDS.  Before the products of a stage's last step:
+//   wait for the next stage (and the reads of this one, which the step before ended with), barrier;
 // then every wave has read stage s, so its place takes stage s + NS: requests run NS - 1 stages ahead, across the tiles
 // of the block, so a tile starts with its operands there, and its output leaves while the next one's arrive.  Requests
 // past the last stage re-read it into places that nothing reads.  The scales, a dword per lane, tile and 256 columns, go
@@ -252,6 +260,10 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {   // the compiler w
   u32x4 v;
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
   return v;
+}
+template <int OFF>
+__device__ __forceinline__ void lds_write16(uint32_t addr, const u32x4& v) {
+  asm volatile("ds_write_b128 %0, %1 offset:%2" ::"v"(addr), "v"(v), "i"(OFF) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_read4(uint32_t addr) {
   uint32_t v;
@@ -268,26 +280,29 @@ template <int FMT, int WGN, int WGM, int FN, int FM>
 struct MxTile {
   static constexpr int XU = FMT == E2M1 ? 1 : 2;
   static constexpr int TN = WGN * FN, TM = WGM * FM, NW = WGN * WGM;
-  static constexpr int STAGE = (TN + TM * XU) * 1024;                         // bytes
+  static constexpr int STEP = (TN + TM * XU) * 1024;                         // bytes
+  // Large tiles gain from requests in small pieces; the smallest from fewer barriers (320 rows of 5120 x 5120, e2m1, 4 x 2
+  // tiles: 15.5 us with four steps to a stage, 18.4 with one).
+  static constexpr int CS = STEP <= 6 * 1024 ? 4 : 1, STAGE = CS * STEP, SPQ = 4 / CS;   // stages of a quad
   static constexpr int SCALES = (TN + TM) * 256, SR = 4;                     // of a quad; quads in the ring
   static constexpr int UNITS = STAGE / 1024, PER = (UNITS + NW - 1) / NW;    // 1 KB requests of a stage, of a wave
   static constexpr int SPER = (TN + TM + NW - 1) / NW;                       // requests of a quad's scales, of a wave
   static constexpr int PAD = 36;                                             // floats of a row of the epilogue's tile
   static constexpr int OUT = NW * 32 * PAD * 4;
   static constexpr int most(int a, int b) { return a < b ? a : b; }
-  static constexpr int NS = most(most((160 * 1024 - SR * SCALES - OUT) / STAGE, (56 - 3 * SPER) / PER), MX_MAX_STAGES);
+  static constexpr int NS = most(most((160 * 1024 - SR * SCALES - OUT) / STAGE, (56 - 3 * SPER) / PER), most(MX_MAX_STAGES, SR * SPQ));
   static constexpr int LDS = SR * SCALES + NS * STAGE + OUT;
-  // requests of scales in the last n steps before step j of a quad (one at each step 0, before the stage's own)
-  static constexpr int scale_requests(int j, int n) { return n >= j ? (n - j) / 4 + (j > 0) : 0; }
+  // requests of scales with the n stages before stage j of a quad (one with each quad's first, before the stage's own)
+  static constexpr int scale_requests(int j, int n) { return j > 0 ? (n >= j ? (n - j) / SPQ + 1 : 0) : n / SPQ; }
 };
 
-template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
+template <int FMT, bool EXACT, bool GLU, int WGN, int WGM, int FN, int FM>
 __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs p, int tiles_m, int tiles_n, int splits) {
   using T = MxTile<FMT, WGN, WGM, FN, FM>;
-  constexpr int XU = T::XU, TN = T::TN, TM = T::TM, NW = T::NW, NS = T::NS, STAGE = T::STAGE;
+  constexpr int XU = T::XU, TN = T::TN, TM = T::TM, NW = T::NW, NS = T::NS, CS = T::CS, STEP = T::STEP, STAGE = T::STAGE;
   constexpr int UNITS = T::UNITS, PER = T::PER, SPER = T::SPER, SR = T::SR;
-  constexpr int NR = FN + FM * XU, NM = FN * FM;                             // LDS reads and products of a stage
-  static_assert(NS >= 3 && NS <= 4 * SR, "ring");
+  constexpr int NR = FN + FM * XU, NM = FN * FM;                             // LDS reads and products of a step
+  static_assert(NS >= 3 && NS <= T::SPQ * SR, "ring");
   extern __shared__ uint4 lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave % WGN, wm = wave / WGN;
@@ -302,53 +317,56 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
   };
   auto place = [&](int t) {
     constexpr int GM = 8;
-    Place a;
-    a.split = t / (tiles_m * tiles_n);
-    t -= a.split * (tiles_m * tiles_n);
-    const int group = t / (GM * tiles_n), in = t % (GM * tiles_n), gm = min(GM, tiles_m - group * GM);
-    a.tm = group * GM + in % gm;
-    a.tn = in / gm;
-    a.q0 = (int)((long)p.quads * a.split / splits);
-    a.quads = (int)((long)p.quads * (a.split + 1) / splits) - a.q0;
+    Place a{0, 0, 0, 0, p.quads};
+    if (splits > 1) {
+      a.split = t / (tiles_m * tiles_n);
+      t -= a.split * (tiles_m * tiles_n);
+      a.q0 = p.quads * a.split / splits;
+      a.quads = p.quads * (a.split + 1) / splits - a.q0;
+    }
+    const int group = tiles_m > GM ? t / (GM * tiles_n) : 0, gm = min(GM, tiles_m - group * GM);
+    t -= group * (GM * tiles_n);
+    a.tn = t / gm;
+    a.tm = group * GM + t - a.tn * gm;
     return a;
   };
 
-  // requests: unit j * NW + wave of a stage: W tiles, then x tiles (e4m3: two units)
+  // requests: unit j * NW + wave of a stage: [step][W tiles, then x tiles (e4m3: two units)]
   const char* src[PER];
-  int r_tile = t_first, r_left = 0, r_slot = 0;
+  int r_tile = t_first - stride, r_quads = 0, r_slot = 0;
   auto aim = [&](int t) {                            // the requests' tile
     const Place a = place(t);
-    r_left = a.quads * 4;
+    r_quads = a.quads;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const int i = min(j * NW + wave, UNITS - 1);
+      const int u = min(j * NW + wave, UNITS - 1), k = u / (STEP / 1024), i = u % (STEP / 1024);
       if (i < TN) {
         size_t up;
         const int wt = w_tile(p, a.tn * TN + i, up);
-        src[j] = p.w + up + ((size_t)wt * p.quads + a.q0) * 4096;
+        src[j] = p.w + up + ((size_t)wt * p.quads + a.q0) * 4096 + k * 1024;
       } else {
         const int xt = min(a.tm * TM + (i - TN) / XU, (p.M + 31) / 32 - 1);
-        src[j] = p.a + ((size_t)xt * p.quads + a.q0) * 4096 * XU + ((i - TN) % XU) * 1024;
+        src[j] = p.a + ((size_t)xt * p.quads + a.q0) * 4096 * XU + (k * XU + (i - TN) % XU) * 1024;
       }
     }
   };
   auto request = [&](int j) {
     const int u = min(j * NW + wave, UNITS - 1);
     dma16(src[j] + lane * 16, lds + (SR * T::SCALES + r_slot * STAGE + u * 1024) / 16);
-    src[j] += u < TN ? 1024 : 1024 * XU;
+    src[j] += u % (STEP / 1024) < TN ? CS * 1024 : CS * 1024 * XU;
   };
-  auto requested = [&]() {                           // a stage: on to the next, or the next tile's first
-    r_slot = r_slot + 1 == NS ? 0 : r_slot + 1;
-    if (--r_left == 0) {
+  auto next_quad = [&]() {                           // before a quad's first request: the next tile's after a tile's last
+    if (r_quads == 0) {
       if (r_tile + stride < t_end) r_tile += stride;
       aim(r_tile);
     }
+    --r_quads;
   };
   const char* ssrc[SPER];
-  int s_tile = t_first, s_left = 0, s_slot = 0;
+  int s_tile = t_first - stride, s_quads = 0, s_slot = 0;
   auto aim_scales = [&](int t) {
     const Place a = place(t);
-    s_left = a.quads;
+    s_quads = a.quads;
 #pragma unroll
     for (int j = 0; j < SPER; ++j) {
       const int u = min(j * NW + wave, TN + TM - 1);
@@ -358,31 +376,31 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
     }
   };
   auto request_scales = [&]() {
+    if (s_quads == 0) {
+      if (s_tile + stride < t_end) s_tile += stride;
+      aim_scales(s_tile);
+    }
+    --s_quads;
 #pragma unroll
     for (int j = 0; j < SPER; ++j) {
       dma4(ssrc[j] + lane * 4, lds + (s_slot * T::SCALES + min(j * NW + wave, TN + TM - 1) * 256) / 16);
       ssrc[j] += 256;
     }
     s_slot = (s_slot + 1) % SR;
-    if (--s_left == 0) {
-      if (s_tile + stride < t_end) s_tile += stride;
-      aim_scales(s_tile);
-    }
   };
 
   floatx16 acc[FN][FM];
-  const bool glu = p.kind == SARATHI_LINEAR_SWIGLU;
   // this lane's place in the W tiles, in fragments of a tile (16 bytes of codes, 4 of scales), and in the x tiles
-  const int wplace = FN == 1 && glu ? ((wn & ~1) + (lane >> 4 & 1)) * 64 + (lane & 32) + (lane & 15) + 16 * (wn & 1)
+  const int wplace = FN == 1 && GLU ? ((wn & ~1) + (lane >> 4 & 1)) * 64 + (lane & 32) + (lane & 15) + 16 * (wn & 1)
                                     : wn * FN * 64 + lane;
   const int xplace = (TN + wm * FM * XU) * 64 + lane, xsplace = (TN + wm * FM) * 64 + lane;
   const uint32_t s0 = (uint32_t)(uintptr_t)lds, l0 = s0 + SR * T::SCALES;
   const uint32_t wl = l0 + wplace * 16, xl = l0 + xplace * 16;
-  u32x4 fr[2][NR];                                   // fragments of a stage: W, then x
-  auto read = [&](auto buf, uint32_t at, auto r) {   // fragment r of the stage at `at`
-    constexpr int B = decltype(buf)::value, R = decltype(r)::value;
-    if constexpr (R < FN) fr[B][R] = lds_read16<R * 1024>(wl + at);
-    else fr[B][R] = lds_read16<(R - FN) * 1024>(xl + at);
+  u32x4 fr[2][NR];                                   // fragments of a step: W, then x
+  auto read = [&](auto buf, auto k, uint32_t at, auto r) {   // fragment r of step k of the stage at `at`
+    constexpr int B = decltype(buf)::value, K = decltype(k)::value, R = decltype(r)::value;
+    if constexpr (R < FN) fr[B][R] = lds_read16<K * STEP + R * 1024>(wl + at);
+    else fr[B][R] = lds_read16<K * STEP + (R - FN) * 1024>(xl + at);
   };
   uint32_t sc[FN + FM], sc_next[FN + FM];            // the quad's scales: W, then x
   int sc_slot = 0;
@@ -396,46 +414,51 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
   using C1 = std::integral_constant<int, 1>;
   auto landed = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
 
-  aim(t_first);
-  aim_scales(t_first);
-  static_for<0, 4 * SR>([&](auto t) {                // steps -4 SR .. -1: at step s, stage s + NS; at 4 q, scales of quad q + SR
-    constexpr int S = decltype(t)::value - 4 * SR;
-    if constexpr (S % 4 == 0) request_scales();
-    if constexpr (S >= -NS) {
+  // The loop's order, from stage -SPQ SR on: at stage s, requests of stage s + NS; at a quad's first, scales SR quads
+  // ahead.  (Not unrolled: the copies' code, fetched once each, took 7 to 12 us of a launch.)
+#pragma unroll 1
+  for (int t = -T::SPQ * SR; t < 0; ++t) {
+    if (t % T::SPQ == 0) request_scales();
+    if (t < -NS) continue;
+    if ((t + NS) % T::SPQ == 0) next_quad();
 #pragma unroll
-      for (int j = 0; j < PER; ++j) request(j);
-      requested();
-    }
-  });
-  wait_vmcnt<(NS - 1) * PER + (NS - 1) / 4 * SPER>();   // quad 0's scales and stage 0
+    for (int j = 0; j < PER; ++j) request(j);
+    r_slot = r_slot + 1 == NS ? 0 : r_slot + 1;
+  }
+  wait_vmcnt<(NS - 1) * PER + (NS - 1) / T::SPQ * SPER>();   // quad 0's scales and stage 0
   lds_barrier();
   read_scales(sc);
-  static_for<0, NR>([&](auto r) { read(C0{}, 0, r); });
+  static_for<0, NR>([&](auto r) { read(C0{}, C0{}, 0, r); });
   landed();
   pin_regs(sc);
   pin_regs(fr[0]);
 
   int slot = 0;
-  auto stage = [&](auto jc) {                        // J of a quad's four
-    constexpr int J = decltype(jc)::value, B = J & 1;
+  auto step = [&](auto jc) {                         // J of a quad's four
+    constexpr int J = decltype(jc)::value, B = J & 1, SP = J / CS;   // the stage's place in its quad
+    constexpr bool LAST = J % CS == CS - 1;
     const int next = slot + 1 == NS ? 0 : slot + 1;
-    // stage s + 1: younger are the requests of NS - 2 stages, with those of a quad's scales before some
-    wait_vmcnt<(NS - 2) * PER + T::scale_requests(J, NS - 2) * SPER>();
-    lds_barrier();
-    if constexpr (J == 0) request_scales();
+    const uint32_t at = (LAST ? next : slot) * STAGE;
+    if constexpr (LAST) {
+      // the next stage: younger are the requests of NS - 2 stages, with those of scales before some
+      wait_vmcnt<(NS - 2) * PER + T::scale_requests(SP, NS - 2) * SPER>();
+      lds_barrier();
+      if constexpr (SP == 0) request_scales();
+      if constexpr ((SP + NS) % T::SPQ == 0) next_quad();
+    }
     static_for<0, NM>([&](auto i) {
       constexpr int I = decltype(i)::value, fm = I / FN, fn = I % FN;
       acc[fn][fm] = mx_mfma<FMT, EXACT, J>(fr[B][fn], sc[fn], &fr[B][FN + fm * XU], sc[FN + fm], acc[fn][fm]);
-      // the next stage's reads in the first three quarters of the products, requests beside all of them
+      // the next step's reads in the first three quarters of the products, requests beside all of them
       constexpr int SPREAD = (NM * 3 + 3) / 4, R0 = I * NR / SPREAD, R1 = (I + 1) * NR / SPREAD;
-      static_for<(R0 < NR ? R0 : NR), (R1 < NR ? R1 : NR)>(
-          [&](auto r) { read(std::integral_constant<int, 1 - B>{}, next * STAGE, r); });
-      static_for<I * PER / NM, (I + 1) * PER / NM>([&](auto j) { request(decltype(j)::value); });
+      static_for<(R0 < NR ? R0 : NR), (R1 < NR ? R1 : NR)>([&](auto r) {
+        read(std::integral_constant<int, 1 - B>{}, std::integral_constant<int, LAST ? 0 : J % CS + 1>{}, at, r);
+      });
+      if constexpr (LAST) static_for<I * PER / NM, (I + 1) * PER / NM>([&](auto j) { request(decltype(j)::value); });
       if constexpr (J == 3 && I == 0) read_scales(sc_next);
       __builtin_amdgcn_sched_barrier(0);
     });
-    requested();
-    slot = next;
+    if constexpr (LAST) slot = r_slot = next;          // the places run together
     landed();
     pin_regs(fr[1 - B]);
     if constexpr (J == 3) {
@@ -445,7 +468,7 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
     }
   };
 
-  float* out = reinterpret_cast<float*>(lds + (SR * T::SCALES + NS * STAGE) / 16) + wave * (32 * T::PAD);
+  const uint32_t out = (uint32_t)(uintptr_t)lds + SR * T::SCALES + NS * STAGE + wave * (32 * T::PAD * 4);
   for (int t = t_first; t < t_end; t += stride) {
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -454,40 +477,73 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
 #pragma unroll
         for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
     const Place at = place(t);
-    for (int q = 0; q < at.quads; ++q) static_for<0, 4>([&](auto j) { stage(j); });
+    for (int q = 0; q < at.quads; ++q) static_for<0, 4>([&](auto j) { step(j); });
 
-    // The output, 32 rows by W (16 or 32) columns at a time through the wave's part of LDS, so that it leaves in larger
-    // pieces of its rows.
-    auto leave = [&](auto width, auto count, auto&& value) {   // value(f, fm, k): element k of the wave's output tile f
-      constexpr int W = decltype(width)::value, FO = decltype(count)::value, PR = 256 / W;   // rows that leave at once
-      static_for<0, FM * FO>([&](auto ic) {
-        constexpr int I = decltype(ic)::value, fm = I / FO, f = I % FO;
+    // The output: SwiGLU in place, then a piece of 32 rows by 32 (FN = 1, SwiGLU: 16) columns at a time through the
+    // wave's part of LDS, so that it leaves in larger pieces of its rows.  One copy of the code that stores a piece: the
+    // whole of it unrolled is fetched anew for every tile (10 to 20 thousand cycles).  LDS by hand here too, or the
+    // compiler would wait for the stores of one piece before the next; a piece's residual is requested before the piece
+    // in front of it is stored.
+    constexpr int FO = GLU ? (FN + 1) / 2 : FN, PIECES = FO * FM;   // output tiles of the wave, side by side
+    constexpr int W = FN == 1 && GLU ? 16 : 32, PR = 256 / W, ROWS = 32 / PR;   // columns of one; rows that leave at once
+    if constexpr (GLU) {
 #pragma unroll
-        for (int g = 0; g < W / 8; ++g)
-          *reinterpret_cast<float4*>(out + (lane & 31) * T::PAD + 8 * g + 4 * (lane >> 5)) =
-              make_float4(value(f, fm, 4 * g), value(f, fm, 4 * g + 1), value(f, fm, 4 * g + 2), value(f, fm, 4 * g + 3));
-        const int r = lane / (W / 4), c = lane % (W / 4) * 4;
-        const int m = (at.tm * TM + wm * FM + fm) * 32 + r, n = ((at.tn * WGN + wn) * FO + f) * W + c;
+      for (int g = 0; g < FM; ++g)
 #pragma unroll
-        for (int i = 0; i < 32; i += PR) {
-          const float4 v = *reinterpret_cast<const float4*>(out + (r + i) * T::PAD + c);
-          if (splits == 1) mx_store4(p, m + i, n, v);
-          else if (m + i < p.M && n < p.N) *reinterpret_cast<float4*>(p.parts + ((size_t)at.split * p.M + m + i) * p.N + n) = v;
-        }
-      });
+        for (int f = 0; f < FO; ++f)
+#pragma unroll
+          for (int k = 0; k < W / 2; ++k)
+            acc[f][g][k] = FN == 1 ? swiglu_f(acc[0][g][k], acc[0][g][k + 8 & 15])
+                                   : swiglu_f(acc[2 * f % FN][g][k], acc[(2 * f + 1) % FN][g][k]);
+    }
+    const int r0 = lane / (W / 4), c0 = lane % (W / 4) * 4;
+    const int m0 = (at.tm * TM + wm * FM) * 32 + r0, n0 = (at.tn * WGN + wn) * FO * W + c0;
+    const uint32_t put_at = out + ((lane & 31) * T::PAD + 4 * (lane >> 5)) * 4, get_at = out + (r0 * T::PAD + c0) * 4;
+    const bool add = !GLU && splits == 1 && adds_resid(p) && p.N % 4 == 0;
+    float4 res[ROWS];
+    auto load_res = [&](int piece) {
+      const int m = m0 + piece / FO * 32, n = n0 + piece % FO * W;
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i)
+        if (m + i * PR < p.M && n < p.N) res[i] = load_resid4(p, m + i * PR, n);
     };
-    using W32 = std::integral_constant<int, 32>;
-    if (glu) {
-      if constexpr (FN == 1)
-        leave(std::integral_constant<int, 16>{}, C1{},
-              [&](int, int fm, int k) { return swiglu_f(acc[0][fm][k], acc[0][fm][k + 8]); });
-      else
-        leave(W32{}, std::integral_constant<int, FN / 2>{},
-              [&](int f, int fm, int k) { return swiglu_f(acc[2 * f][fm][k], acc[2 * f + 1][fm][k]); });
-    } else if (p.kind == SARATHI_LINEAR_GELU && splits == 1) {
-      leave(W32{}, std::integral_constant<int, FN>{}, [&](int f, int fm, int k) { return gelu_f(acc[f][fm][k]); });
-    } else {
-      leave(W32{}, std::integral_constant<int, FN>{}, [&](int f, int fm, int k) { return acc[f][fm][k]; });
+    if (add) load_res(0);
+#pragma unroll 1
+    for (int piece = 0; piece < PIECES; ++piece) {
+      static_for<0, PIECES>([&](auto ic) {
+        constexpr int I = decltype(ic)::value;
+        if (piece != I) return;
+        static_for<0, W / 8>([&](auto gc) {
+          constexpr int G = decltype(gc)::value;
+          const floatx16& a = acc[I % FO][I / FO];
+          const float v[4] = {a[4 * G], a[4 * G + 1], a[4 * G + 2], a[4 * G + 3]};
+          lds_write16<G * 32>(put_at, __builtin_bit_cast(u32x4, v));
+        });
+      });
+      u32x4 v[ROWS];
+      static_for<0, ROWS>([&](auto rc) { v[decltype(rc)::value] = lds_read16<decltype(rc)::value * PR * T::PAD * 4>(get_at); });
+      landed();
+      pin_regs(v);
+      if (add) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) v[i] = __builtin_bit_cast(u32x4, add4(__builtin_bit_cast(float4, v[i]), res[i]));
+        if (piece + 1 < PIECES) load_res(piece + 1);
+      } else if (!GLU && splits == 1 && p.kind == SARATHI_LINEAR_GELU) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[i][e] = __float_as_uint(gelu_f(__uint_as_float(v[i][e])));
+      }
+      const int m = m0 + piece / FO * 32, n = n0 + piece % FO * W;
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const int row = m + i * PR;
+        if (row >= p.M || n >= p.N) continue;
+        const float4 y = __builtin_bit_cast(float4, v[i]);
+        if (!GLU && splits > 1) *reinterpret_cast<float4*>(p.parts + ((size_t)at.split * p.M + row) * p.N + n) = y;
+        else if (p.N % 4) put_any(p, row, n, y);
+        else put4(p, row, n, y);
+      }
     }
   }
   wait_vmcnt<0>();                                   // requests past the last tile still fill the stages
@@ -513,14 +569,14 @@ size_t mx_linear_parts(int M, int N) {
   return std::min((size_t)MX_MAX_SPLITS * M * N, (size_t)256 * 65536);
 }
 
-template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
-static hipError_t run_tile(const MxLinearArgs& a, int splits, hipStream_t s) {
+template <int FMT, bool EXACT, bool GLU, int WGN, int WGM, int FN, int FM>
+static hipError_t run_tile_as(const MxLinearArgs& a, int splits, hipStream_t s) {
   using T = MxTile<FMT, WGN, WGM, FN, FM>;
-  const auto kernel = mx_tile_kernel<FMT, EXACT, WGN, WGM, FN, FM>;
+  const auto kernel = mx_tile_kernel<FMT, EXACT, GLU, WGN, WGM, FN, FM>;
   static std::atomic<uint64_t> lds_set{0};           // devices on which this instance's LDS limit is raised
   hipError_t e = ensure_dynamic_lds((const void*)kernel, T::LDS, lds_set);
   if (e != hipSuccess) return e;
-  const int w_tiles = (a.kind == SARATHI_LINEAR_SWIGLU ? 2 : 1) * mx_tiles(a.N);
+  const int w_tiles = (GLU ? 2 : 1) * mx_tiles(a.N);
   const int tiles_n = (w_tiles + T::TN - 1) / T::TN, tiles_m = (mx_tiles(a.M) + T::TM - 1) / T::TM;
   const int grid = std::min((tiles_n * tiles_m * splits + 7) / 8 * 8, 256);   // a block per CU
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * T::NW), T::LDS, s, a, tiles_m, tiles_n, splits);
@@ -528,6 +584,12 @@ static hipError_t run_tile(const MxLinearArgs& a, int splits, hipStream_t s) {
   if (e != hipSuccess || splits == 1) return e;
   hipLaunchKernelGGL(mx_join_kernel, dim3((unsigned)(((size_t)a.M * a.N / 4 + 255) / 256)), dim3(256), 0, s, a, splits);
   return hipGetLastError();
+}
+
+template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
+static hipError_t run_tile(const MxLinearArgs& a, int splits, hipStream_t s) {
+  return a.kind == SARATHI_LINEAR_SWIGLU ? run_tile_as<FMT, EXACT, true, WGN, WGM, FN, FM>(a, 1, s)
+                                         : run_tile_as<FMT, EXACT, false, WGN, WGM, FN, FM>(a, splits, s);
 }
 
 template <int FMT, bool EXACT, int NW, int FN, int FM>
