@@ -482,8 +482,7 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
     // The output: SwiGLU in place, then a piece of 32 rows by 32 (FN = 1, SwiGLU: 16) columns at a time through the
     // wave's part of LDS, so that it leaves in larger pieces of its rows.  One copy of the code that stores a piece: the
     // whole of it unrolled is fetched anew for every tile (10 to 20 thousand cycles).  LDS by hand here too, or the
-    // compiler would wait for the stores of one piece before the next; a piece's residual is requested before the piece
-    // in front of it is stored.
+    // compiler would wait for the stores of one piece before the next.
     constexpr int FO = GLU ? (FN + 1) / 2 : FN, PIECES = FO * FM;   // output tiles of the wave, side by side
     constexpr int W = FN == 1 && GLU ? 16 : 32, PR = 256 / W, ROWS = 32 / PR;   // columns of one; rows that leave at once
     if constexpr (GLU) {
@@ -496,18 +495,12 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
             acc[f][g][k] = FN == 1 ? swiglu_f(acc[0][g][k], acc[0][g][k + 8 & 15])
                                    : swiglu_f(acc[2 * f % FN][g][k], acc[(2 * f + 1) % FN][g][k]);
     }
-    const int r0 = lane / (W / 4), c0 = lane % (W / 4) * 4;
+    int le = threadIdx.x & 63;                       // the lane anew: what follows from it needs no register in the loop
+    asm volatile("" : "+v"(le));
+    const int r0 = le / (W / 4), c0 = le % (W / 4) * 4;
     const int m0 = (at.tm * TM + wm * FM) * 32 + r0, n0 = (at.tn * WGN + wn) * FO * W + c0;
-    const uint32_t put_at = out + ((lane & 31) * T::PAD + 4 * (lane >> 5)) * 4, get_at = out + (r0 * T::PAD + c0) * 4;
+    const uint32_t put_at = out + ((le & 31) * T::PAD + 4 * (le >> 5)) * 4, get_at = out + (r0 * T::PAD + c0) * 4;
     const bool add = !GLU && splits == 1 && adds_resid(p) && p.N % 4 == 0;
-    float4 res[ROWS];
-    auto load_res = [&](int piece) {
-      const int m = m0 + piece / FO * 32, n = n0 + piece % FO * W;
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i)
-        if (m + i * PR < p.M && n < p.N) res[i] = load_resid4(p, m + i * PR, n);
-    };
-    if (add) load_res(0);
 #pragma unroll 1
     for (int piece = 0; piece < PIECES; ++piece) {
       static_for<0, PIECES>([&](auto ic) {
@@ -524,17 +517,19 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
       static_for<0, ROWS>([&](auto rc) { v[decltype(rc)::value] = lds_read16<decltype(rc)::value * PR * T::PAD * 4>(get_at); });
       landed();
       pin_regs(v);
+      const int m = m0 + piece / FO * 32, n = n0 + piece % FO * W;
       if (add) {
+        float4 res[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) res[i] = load_resid4(p, min(m + i * PR, p.M - 1), min(n, p.N - 4));
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) v[i] = __builtin_bit_cast(u32x4, add4(__builtin_bit_cast(float4, v[i]), res[i]));
-        if (piece + 1 < PIECES) load_res(piece + 1);
       } else if (!GLU && splits == 1 && p.kind == SARATHI_LINEAR_GELU) {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[i][e] = __float_as_uint(gelu_f(__uint_as_float(v[i][e])));
       }
-      const int m = m0 + piece / FO * 32, n = n0 + piece % FO * W;
 #pragma unroll
       for (int i = 0; i < ROWS; ++i) {
         const int row = m + i * PR;
