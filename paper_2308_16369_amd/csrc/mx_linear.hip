@@ -560,7 +560,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxLinearArgs p, int splits
 // Most that split columns can use: at most 256 tiles run, of 64 K output elements at most; eight splits.
 constexpr int MX_MAX_SPLITS = 8;
 size_t mx_linear_parts(int M, int N) {
-  if (M <= 64) return 0;
+  if (M <= MX_ROWS) return 0;
   return std::min((size_t)MX_MAX_SPLITS * M * N, (size_t)256 * 65536);
 }
 
@@ -594,17 +594,17 @@ static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The tiles of the second kernel, and what 64 columns of one cost on a CU: a fixed part (barrier, waits) and one per
-// product of a W tile and an x tile, in units of 0.14 us (fitted to one round of 80 stages: e2m1 rows 16.6, 17.8, 24.6,
-// 29.4, 31.4, 37.0 us in the order below, e4m3 18.9, 21.8, 30.6, 38.4, 41.2, 52.9).  A launch takes whole rounds of one
-// tile per CU.  Exact products cost twice the matrix instructions and the split of every x fragment, which FN W tiles
-// share.  Where tiles leave CUs idle, the columns are split: shorter tiles, but the partial sums are written and read
-// back, and a launch of their own joins them (320 rows of 5120 x 13824, e2m1: SPLITFIG).
+// The tiles of the second kernel (W tiles by x tiles) and what 64 columns of one cost with every CU busy, in us (from 4096
+// rows of 13824 x 5120, a round of one tile per CU: e2m1 12.1, 15.5, 27.5, 28.8, 32.2, 40 us in the order below, e4m3 14.5,
+// 23.4, 33, 39.6 and 53.7, with exact sums 27, 37, 55 and 98; 2.5 of them the output's).  0: not built, another tile is
+// faster everywhere (the split of an x fragment for exact sums is shared by FN W tiles).  Where tiles leave CUs idle, the
+// columns are split: shorter tiles, but the partial sums are written and read back, and a launch of their own joins them.
 struct TileCost {
   int tn, tm;
-  float exact;
+  float e2m1, e4m3, exact;
 };
-constexpr TileCost kTiles[] = {{4, 2, 0.21f}, {4, 4, 0.18f}, {8, 4, 0.145f}, {4, 10, 0.20f}, {8, 6, 0.143f}, {8, 8, 0.118f}};
+constexpr TileCost kTiles[] = {{4, 2, 0.120f, 0.150f, 0.306f}, {4, 4, 0.160f, 0.260f, 0.430f}, {8, 4, 0.31f, 0.385f, 0.66f},
+                               {4, 10, 0.33f, 0.465f, 0},      {8, 6, 0.37f, 0, 0},            {8, 8, 0.47f, 0.64f, 1.19f}};
 
 struct TilePick {
   int tile, splits;
@@ -617,11 +617,12 @@ static TilePick pick_tile(const MxLinearArgs& a, int w_tiles, int x_tiles, int f
   const bool can_split = a.parts && a.kind != SARATHI_LINEAR_SWIGLU && a.N % 4 == 0;
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const TileCost& t = kTiles[i];
+    const float cost = exact ? t.exact : format == E2M1 ? t.e2m1 : t.e4m3;
+    if (cost == 0) continue;
     const long tiles = (long)((w_tiles + t.tn - 1) / t.tn) * ((x_tiles + t.tm - 1) / t.tm);
     for (int n = 1; n <= MX_MAX_SPLITS; ++n) {
       if (n > 1 && (!can_split || n * tiles > 256 || a.quads < 4 * n || n * size > a.parts_cap)) break;
-      const float stages = (float)((tiles * n + 255) / 256) * ((a.quads + n - 1) / n) * 4;
-      float us = 0.14f * stages * (1.0f + t.tn * t.tm * (exact ? t.exact : format == E2M1 ? 0.037f : 0.057f));
+      float us = (float)((tiles * n + 255) / 256) * (2.5f + ((a.quads + n - 1) / n) * 4 * cost);
       if (n > 1) us += 4.0f + n * size * 8e-6f / 5.0f;   // the launch; partial sums written and read, 5 TB/s
       if (us < least) least = us, best = {i, n};
     }
@@ -633,9 +634,11 @@ template <int FMT, bool EXACT>
 static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s) {
   const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
   const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
-  // Up to 64 rows stream; up to 128 where the W tiles leave CUs idle in the other kernel (128 rows of 5120 x 13824: 29
-  // us, 35 there; of 15360 x 5120 27 and 23).
-  if (x_tiles <= 2 || (x_tiles <= 4 && w_tiles <= 256)) {
+  // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
+  // e2m1: 9.6 us, 14 there).  Not where there are few W tiles and many columns, which the other kernel can split
+  // (STREAMFIG).
+  const bool few = w_tiles <= 256, split = few && a.quads > 32 && a.parts && !glu && a.N % 4 == 0;
+  if (x_tiles == 1 || (x_tiles == 2 && !split) || (x_tiles <= 4 && few && !split)) {
     switch (x_tiles) {
       case 1:
         if (glu) return run_stream<FMT, EXACT, 8, 2, 1>(a, s);
@@ -652,10 +655,12 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s) {
   const TilePick pick = pick_tile(a, w_tiles, x_tiles, FMT, EXACT);
   switch (pick.tile) {
     case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, pick.splits, s);
-    case 1: return run_tile<FMT, EXACT, 4, 2, 1, 2>(a, pick.splits, s);
-    case 2: return run_tile<FMT, EXACT, 4, 2, 2, 2>(a, pick.splits, s);
-    case 3: return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, pick.splits, s);
-    case 4: return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, pick.splits, s);
+    case 1: return run_tile<FMT, EXACT, 2, 4, 2, 1>(a, pick.splits, s);
+    case 2: return run_tile<FMT, EXACT, 2, 4, 4, 1>(a, pick.splits, s);
+    case 3:
+      if constexpr (!EXACT) return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, pick.splits, s);
+    case 4:
+      if constexpr (FMT == E2M1) return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, pick.splits, s);
     default: return run_tile<FMT, EXACT, 2, 4, 4, 2>(a, pick.splits, s);
   }
 }
