@@ -112,6 +112,11 @@ int sarathi_mx_norm(int stream_dtype, int dtype, int format, int rows, int cols,
  * K not a multiple of 8, more than 2^24 - 1 tiles), EHIP.
  */
 size_t sarathi_mx_linear_scratch_bytes(int M, int N);
+/* What sarathi_mx_linear would run with scratch_bytes of scratch, as sarathi_linear_plan: *bm rows of a by *bn rows of w
+ * (SwiGLU: gate and up rows together) to a block, the columns in *n_split shares.  Nothing is launched.  Errors: EINVAL
+ * (NULL outputs, kind, sizes), EUNSUPPORTED as below. */
+int sarathi_mx_linear_plan(int dtype, int kind, int a_format, int M, int N, int K, size_t scratch_bytes, int* bm,
+                           int* bn, int* n_split);
 int sarathi_mx_linear(int dtype, int kind, int a_format, int M, int N, int K, const void* a, const void* w,
                       const void* resid, void* out, void* scratch, size_t scratch_bytes, void* hip_stream);
 

@@ -57,7 +57,11 @@ struct MxLinearArgs {
   float* parts;            // [split][M][N], or NULL
   size_t parts_cap;        // floats
 };
-hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s);
+struct MxLinearPlan {
+  int bm, bn, splits;      // rows of x and W rows of a block, shares of the columns
+};
+// With `plan`, nothing is launched: what would run.
+hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s, MxLinearPlan* plan = nullptr);
 size_t mx_linear_parts(int M, int N);   // floats that the launch can use
 
 }  // namespace sarathi

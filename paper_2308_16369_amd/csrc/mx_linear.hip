@@ -568,6 +568,7 @@ template <int FMT, bool EXACT, bool GLU, int WGN, int WGM, int FN, int FM>
 static hipError_t run_tile_as(const MxLinearArgs& a, int splits, hipStream_t s) {
   using T = MxTile<FMT, WGN, WGM, FN, FM>;
   const auto kernel = mx_tile_kernel<FMT, EXACT, GLU, WGN, WGM, FN, FM>;
+  static_assert(T::LDS <= 160 * 1024, "LDS of a CU");
   static std::atomic<uint64_t> lds_set{0};           // devices on which this instance's LDS limit is raised
   hipError_t e = ensure_dynamic_lds((const void*)kernel, T::LDS, lds_set);
   if (e != hipSuccess) return e;
@@ -582,13 +583,21 @@ static hipError_t run_tile_as(const MxLinearArgs& a, int splits, hipStream_t s) 
 }
 
 template <int FMT, bool EXACT, int WGN, int WGM, int FN, int FM>
-static hipError_t run_tile(const MxLinearArgs& a, int splits, hipStream_t s) {
+static hipError_t run_tile(const MxLinearArgs& a, int splits, hipStream_t s, MxLinearPlan* plan) {
+  if (plan) {
+    *plan = {WGM * FM * MX_ROWS, WGN * FN * MX_ROWS, splits};
+    return hipSuccess;
+  }
   return a.kind == SARATHI_LINEAR_SWIGLU ? run_tile_as<FMT, EXACT, true, WGN, WGM, FN, FM>(a, 1, s)
                                          : run_tile_as<FMT, EXACT, false, WGN, WGM, FN, FM>(a, splits, s);
 }
 
 template <int FMT, bool EXACT, int NW, int FN, int FM>
-static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s) {
+static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* plan) {
+  if (plan) {
+    *plan = {FM * MX_ROWS, FN * MX_ROWS, 1};
+    return hipSuccess;
+  }
   const int w_tiles = (a.kind == SARATHI_LINEAR_SWIGLU ? 2 : 1) * mx_tiles(a.N);
   hipLaunchKernelGGL((mx_stream_kernel<FMT, EXACT, NW, FN, FM>), dim3((w_tiles + FN - 1) / FN), dim3(64 * NW), 0, s, a);
   return hipGetLastError();
@@ -631,7 +640,7 @@ static TilePick pick_tile(const MxLinearArgs& a, int w_tiles, int x_tiles, int f
 }
 
 template <int FMT, bool EXACT>
-static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s) {
+static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* plan) {
   const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
   const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
   // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
@@ -641,34 +650,34 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s) {
   if (x_tiles == 1 || (x_tiles == 2 && !split) || (x_tiles <= 4 && few && !split)) {
     switch (x_tiles) {
       case 1:
-        if (glu) return run_stream<FMT, EXACT, 8, 2, 1>(a, s);
-        return w_tiles <= 256 ? run_stream<FMT, EXACT, 16, 1, 1>(a, s) : run_stream<FMT, EXACT, 8, 1, 1>(a, s);
+        if (glu) return run_stream<FMT, EXACT, 8, 2, 1>(a, s, plan);
+        return w_tiles <= 256 ? run_stream<FMT, EXACT, 16, 1, 1>(a, s, plan) : run_stream<FMT, EXACT, 8, 1, 1>(a, s, plan);
       case 2:
-        if (glu) return run_stream<FMT, EXACT, 8, 2, 2>(a, s);
+        if (glu) return run_stream<FMT, EXACT, 8, 2, 2>(a, s, plan);
         if constexpr (FMT == E2M1)                    // (e4m3: the registers of 16 waves do not hold a quad)
-          if (w_tiles <= 256) return run_stream<FMT, EXACT, 16, 1, 2>(a, s);
-        return run_stream<FMT, EXACT, 8, 1, 2>(a, s);
-      case 3: return glu ? run_stream<FMT, EXACT, 4, 2, 3>(a, s) : run_stream<FMT, EXACT, 8, 1, 3>(a, s);
-      default: return glu ? run_stream<FMT, EXACT, 4, 2, 4>(a, s) : run_stream<FMT, EXACT, 4, 1, 4>(a, s);
+          if (w_tiles <= 256) return run_stream<FMT, EXACT, 16, 1, 2>(a, s, plan);
+        return run_stream<FMT, EXACT, 8, 1, 2>(a, s, plan);
+      case 3: return glu ? run_stream<FMT, EXACT, 4, 2, 3>(a, s, plan) : run_stream<FMT, EXACT, 8, 1, 3>(a, s, plan);
+      default: return glu ? run_stream<FMT, EXACT, 4, 2, 4>(a, s, plan) : run_stream<FMT, EXACT, 4, 1, 4>(a, s, plan);
     }
   }
   const TilePick pick = pick_tile(a, w_tiles, x_tiles, FMT, EXACT);
   switch (pick.tile) {
-    case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, pick.splits, s);
-    case 1: return run_tile<FMT, EXACT, 2, 4, 2, 1>(a, pick.splits, s);
-    case 2: return run_tile<FMT, EXACT, 2, 4, 4, 1>(a, pick.splits, s);
+    case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, pick.splits, s, plan);
+    case 1: return run_tile<FMT, EXACT, 2, 4, 2, 1>(a, pick.splits, s, plan);
+    case 2: return run_tile<FMT, EXACT, 2, 4, 4, 1>(a, pick.splits, s, plan);
     case 3:
-      if constexpr (!EXACT) return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, pick.splits, s);
+      if constexpr (!EXACT) return run_tile<FMT, EXACT, 4, 2, 1, 5>(a, pick.splits, s, plan);
     case 4:
-      if constexpr (FMT == E2M1) return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, pick.splits, s);
-    default: return run_tile<FMT, EXACT, 2, 4, 4, 2>(a, pick.splits, s);
+      if constexpr (FMT == E2M1) return run_tile<FMT, EXACT, 4, 2, 2, 3>(a, pick.splits, s, plan);
+    default: return run_tile<FMT, EXACT, 2, 4, 4, 2>(a, pick.splits, s, plan);
   }
 }
 
-hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s) {
+hipError_t launch_mx_linear(int a_format, const MxLinearArgs& a, hipStream_t s, MxLinearPlan* plan) {
   const bool f32_out = a.dtype == SARATHI_F32 || a.kind == SARATHI_LINEAR_RESID;
-  if (a_format == E2M1) return linear_as<E2M1, false>(a, s);
-  return f32_out ? linear_as<E4M3, true>(a, s) : linear_as<E4M3, false>(a, s);
+  if (a_format == E2M1) return linear_as<E2M1, false>(a, s, plan);
+  return f32_out ? linear_as<E4M3, true>(a, s, plan) : linear_as<E4M3, false>(a, s, plan);
 }
 
 }  // namespace sarathi

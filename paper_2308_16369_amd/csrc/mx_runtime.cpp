@@ -55,6 +55,17 @@ int check_memory(int format, int rows, int cols, const void* operand, size_t byt
   return SARATHI_OK;
 }
 
+int check_linear(int dtype, int kind, int a_format, int M, int N, int K) {
+  if (!known_dtype(dtype)) return fail(SARATHI_EUNSUPPORTED, "dtype %d", dtype);
+  if (kind < SARATHI_LINEAR_PLAIN || kind > SARATHI_LINEAR_GELU) return fail(SARATHI_EINVAL, "kind %d", kind);
+  if (!known_format(a_format)) return fail(SARATHI_EUNSUPPORTED, "a_format %d", a_format);
+  if (M < 1 || N < 1 || K < 1) return fail(SARATHI_EINVAL, "M, N, K must be positive");
+  if (K % 8) return fail(SARATHI_EUNSUPPORTED, "K %d must be a multiple of 8", K);
+  if (!sizes_fit(M, K) || !sizes_fit(N, K) || (long)mx_tiles(M) * mx_tiles(N) > MAX_TILES)
+    return fail(SARATHI_EUNSUPPORTED, "%d x %d x %d is more than %ld tiles", M, N, K, MAX_TILES);
+  return SARATHI_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -146,15 +157,26 @@ size_t sarathi_mx_linear_scratch_bytes(int M, int N) {
   return mx_linear_parts(M, N) * 4;
 }
 
+int sarathi_mx_linear_plan(int dtype, int kind, int a_format, int M, int N, int K, size_t scratch_bytes, int* bm,
+                           int* bn, int* n_split) {
+  if (!bm || !bn || !n_split) return fail(SARATHI_EINVAL, "NULL pointer");
+  const int rc = check_linear(dtype, kind, a_format, M, N, K);
+  if (rc) return rc;
+  static float dummy;   // plan only: the scratch is never touched
+  MxLinearArgs p{};
+  p.kind = kind; p.dtype = dtype; p.M = M; p.N = N; p.quads = mx_quads(K);
+  p.parts = scratch_bytes >= 4 ? &dummy : nullptr;
+  p.parts_cap = scratch_bytes / 4;
+  MxLinearPlan pl{};
+  if (launch_mx_linear(a_format, p, nullptr, &pl) != hipSuccess) return fail(SARATHI_EINVAL, "no plan for this op");
+  *bm = pl.bm; *bn = pl.bn; *n_split = pl.splits;
+  return SARATHI_OK;
+}
+
 int sarathi_mx_linear(int dtype, int kind, int a_format, int M, int N, int K, const void* a, const void* w,
                       const void* resid, void* out, void* scratch, size_t scratch_bytes, void* hip_stream) {
-  if (!known_dtype(dtype)) return fail(SARATHI_EUNSUPPORTED, "dtype %d", dtype);
-  if (kind < SARATHI_LINEAR_PLAIN || kind > SARATHI_LINEAR_GELU) return fail(SARATHI_EINVAL, "kind %d", kind);
-  if (!known_format(a_format)) return fail(SARATHI_EUNSUPPORTED, "a_format %d", a_format);
-  if (M < 1 || N < 1 || K < 1) return fail(SARATHI_EINVAL, "M, N, K must be positive");
-  if (K % 8) return fail(SARATHI_EUNSUPPORTED, "K %d must be a multiple of 8", K);
-  if (!sizes_fit(M, K) || !sizes_fit(N, K) || (long)mx_tiles(M) * mx_tiles(N) > MAX_TILES)
-    return fail(SARATHI_EUNSUPPORTED, "%d x %d x %d is more than %ld tiles", M, N, K, MAX_TILES);
+  const int rc = check_linear(dtype, kind, a_format, M, N, K);
+  if (rc) return rc;
   if (!a || !w || !out) return fail(SARATHI_EINVAL, "NULL pointer");
   const bool needs_resid = kind == SARATHI_LINEAR_RESID || kind == SARATHI_LINEAR_RESID_F32IN;
   if (needs_resid && !resid) return fail(SARATHI_EINVAL, "resid is NULL");

@@ -177,6 +177,7 @@ EXPORTS = {
                                    ct.c_size_t, ct.c_void_p, ct.c_size_t, ct.c_void_p, ct.c_void_p, ct.c_size_t,
                                    ct.c_void_p, ct.c_size_t, ct.c_void_p]),
     "sarathi_mx_linear_scratch_bytes": (ct.c_size_t, [ct.c_int, ct.c_int]),
+    "sarathi_mx_linear_plan": (ct.c_int, [ct.c_int] * 6 + [ct.c_size_t] + [ct.POINTER(ct.c_int)] * 3),
     "sarathi_mx_linear": (ct.c_int, [ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_int, ct.c_void_p,
                                      ct.c_void_p, ct.c_void_p, ct.c_void_p, ct.c_void_p, ct.c_size_t, ct.c_void_p]),
     "sarathi_kv8_bytes": (ct.c_size_t, [ct.POINTER(sarathi_kv8_cfg), ct.c_int, ct.c_int]),
@@ -609,6 +610,14 @@ def sarathi_mx_norm(stream_dtype: int, dtype: int, format: int, rows: int, cols:
 
 def sarathi_mx_linear_scratch_bytes(M: int, N: int) -> int:
     return lib().sarathi_mx_linear_scratch_bytes(M, N)
+
+
+def sarathi_mx_linear_plan(dtype: int, kind: int, a_format: int, M: int, N: int, K: int, scratch_bytes: int) -> tuple:
+    """(bm, bn, n_split) of an op."""
+    bm, bn, ns = ct.c_int(), ct.c_int(), ct.c_int()
+    _check(lib().sarathi_mx_linear_plan(dtype, kind, a_format, M, N, K, scratch_bytes, ct.byref(bm), ct.byref(bn),
+                                        ct.byref(ns)))
+    return bm.value, bn.value, ns.value
 
 
 def sarathi_mx_linear(dtype: int, kind: int, a_format: int, M: int, N: int, K: int, a: int, w: int, resid: int, out: int,

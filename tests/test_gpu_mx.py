@@ -250,6 +250,75 @@ def test_linear_of_whole_numbers_is_exact(fmt, M, N, K):
             assert torch.equal(out.cpu(), want.to(out.dtype)), (kind, dtype)
 
 
+# The block (rows of x, W rows, whether the columns are split) that each shape is to run with, so that every one is run:
+# rows that end inside a tile, W rows that do, columns that end inside 256, more tiles than CUs (a block's next tile is
+# requested while it finishes the last).
+PICKS = [
+    ("e2m1", "bf16", "plain", 40, 100, 264, 64, 32, 0), ("e2m1", "bf16", "plain", 130, 100, 264, 64, 128, 0),
+    ("e2m1", "bf16", "gelu", 258, 6660, 264, 128, 128, 0), ("e2m1", "f32", "plain", 258, 14000, 264, 128, 256, 0),
+    ("e2m1", "bf16", "resid_f32in", 1600, 5001, 264, 320, 128, 0), ("e2m1", "bf16", "resid", 1300, 6660, 264, 192, 256, 0),
+    ("e2m1", "bf16", "plain", 2100, 14000, 520, 256, 256, 0), ("e2m1", "bf16", "gelu", 40, 100, 8712, 64, 128, 1),
+    ("e2m1", "bf16", "resid", 130, 5000, 8712, 64, 128, 1), ("e2m1", "f32", "resid_f32in", 70, 3500, 12808, 128, 128, 1),
+    ("e2m1", "bf16", "swiglu", 130, 100, 264, 64, 128, 0), ("e2m1", "bf16", "swiglu", 70, 10000, 264, 128, 128, 0),
+    ("e2m1", "bf16", "swiglu", 130, 10000, 264, 128, 256, 0), ("e2m1", "bf16", "swiglu", 258, 14000, 264, 320, 128, 0),
+    ("e2m1", "f32", "swiglu", 400, 10000, 264, 192, 256, 0), ("e2m1", "bf16", "swiglu", 2100, 7001, 776, 256, 256, 0),
+    ("e4m3", "bf16", "plain", 130, 100, 264, 64, 128, 0), ("e4m3", "bf16", "plain", 258, 6660, 264, 128, 128, 0),
+    ("e4m3", "bf16", "resid_f32in", 258, 14000, 264, 128, 256, 0), ("e4m3", "bf16", "gelu", 1600, 5000, 264, 320, 128, 0),
+    ("e4m3", "bf16", "plain", 2100, 14000, 776, 256, 256, 0), ("e4m3", "bf16", "resid_f32in", 70, 6660, 8712, 64, 128, 1),
+    ("e4m3", "bf16", "plain", 500, 1284, 8712, 128, 128, 1), ("e4m3", "bf16", "swiglu", 70, 10000, 264, 128, 128, 0),
+    ("e4m3", "bf16", "swiglu", 130, 10000, 264, 128, 256, 0), ("e4m3", "bf16", "swiglu", 258, 14000, 264, 320, 128, 0),
+    ("e4m3", "bf16", "swiglu", 2100, 7000, 520, 256, 256, 0),
+    ("e4m3", "f32", "plain", 130, 100, 264, 64, 128, 0), ("e4m3", "bf16", "resid", 258, 6661, 264, 128, 128, 0),
+    ("e4m3", "f32", "gelu", 258, 14000, 264, 128, 256, 0), ("e4m3", "bf16", "resid", 1600, 5000, 776, 256, 256, 0),
+    ("e4m3", "f32", "plain", 130, 100, 2560, 64, 128, 1), ("e4m3", "bf16", "resid", 70, 3500, 8712, 128, 128, 1),
+    ("e4m3", "f32", "resid_f32in", 70, 6660, 8712, 128, 256, 1), ("e4m3", "f32", "swiglu", 70, 10000, 264, 128, 128, 0),
+    ("e4m3", "f32", "swiglu", 130, 10000, 264, 128, 256, 0), ("e4m3", "f32", "swiglu", 2100, 7000, 264, 256, 256, 0),
+]
+
+
+@pytest.mark.parametrize("fmt,dtype,kind,M,N,K,bm,bn,split", PICKS, ids=["-".join(map(str, c[:6])) for c in PICKS])
+def test_every_block_shape(fmt, dtype, kind, M, N, K, bm, bn, split):
+    """Sums that fp32 holds exactly, in every block shape; SwiGLU and GELU within their functions' own roundings."""
+    pick = S.sarathi_mx_linear_plan(DT[dtype][0], KIND[kind], FMT[fmt], M, N, K, S.sarathi_mx_linear_scratch_bytes(M, N))
+    assert (pick[0], pick[1], int(pick[2] > 1)) == (bm, bn, split), pick
+    rng = np.random.default_rng(M + N + K)
+    small = 2.0 ** -10 if kind in ("swiglu", "gelu") else 1.0        # sums of a few units
+
+    def draw(r, c):
+        nb = -(-c // 32)
+        codes = rng.integers(-3, 4, (r, nb, 32), dtype=np.int8).astype(np.float32)
+        return (codes * np.exp2(rng.integers(-1, 2, (r, nb, 1))).astype(np.float32)).reshape(r, -1)[:, :c]
+
+    def held(v, f):                                                  # by the library: bit for bit, as tested above
+        x = torch.from_numpy(np.ascontiguousarray(v)).cuda()
+        n = S.sarathi_mx_bytes(FMT[f], x.shape[0], K)
+        op = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+        S.sarathi_mx_quantize(S.F32, FMT[f], x.shape[0], K, x.data_ptr(), K, op.data_ptr(), n, stream())
+        return op, x.double()
+
+    a, av = held(draw(M, K), fmt)
+    parts = [held(draw(N, K) * np.float32(small), "e2m1") for _ in range(2 if kind == "swiglu" else 1)]
+    w = torch.cat([p[0] for p in parts])
+    assert float((av.abs() @ parts[0][1].abs().T).max()) + 8 < 2 ** 22 * small       # 24 bits of the least product, 2^-2
+    r = resid_of(rng, kind, dtype, M, N, whole=True)
+    z = [av @ p[1].T for p in parts]
+    for scratch in ((True, False) if split else (True,)):
+        out = run_linear(a, w, r, kind, dtype, fmt, M, N, K, scratch=scratch)
+        if kind in ("swiglu", "gelu"):
+            if kind == "swiglu":
+                want = z[0] * torch.sigmoid(z[0]) * z[1]
+                tol = want.abs() * (z[0].abs() + 8) * 2.0 ** -23
+            else:
+                want = z[0] * torch.special.ndtr(z[0])
+                tol = z[0].abs() * 4 * 2.0 ** -23
+            half = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8
+            off = (out.double() - want).abs()
+            assert bool((off <= tol + half * (want.abs() + tol) + 2.0 ** -133).all()), float((off / (tol + half * want.abs() + 1e-30)).max())
+        else:
+            want = z[0] + (r.double() if r is not None else 0.0)
+            assert torch.equal(out, want.to(out.dtype))
+
+
 def bound(av, wv, fmt, exact_sums):
     """What fp32 sums of these products can be off by.  A matrix instruction takes 64 columns: eight groups of eight are
     aligned to the largest term, the accumulator among it, and cut below 24 bits: 9 terms off by 2^-23 of the largest, and

@@ -112,6 +112,25 @@ def test_linear_refuses(kw, code):
     assert S.sarathi_mx_linear(**{**LINEAR, **kw}, check=False) == code, S.sarathi_last_error()
 
 
+def test_linear_plan():
+    assert S.sarathi_mx_linear_scratch_bytes(32, 1 << 20) == 0
+    full = S.sarathi_mx_linear_scratch_bytes(200, 5120)
+    assert 0 < full <= 8 * 200 * 5120 * 4 and S.sarathi_mx_linear_scratch_bytes(4096, 28000) <= 64 << 20
+    args = (S.BF16, S.LINEAR_PLAIN, S.MX_E2M1, 200, 5120, 13824)
+    bm, bn, n = S.sarathi_mx_linear_plan(*args, full)
+    assert n > 1 and n * 200 * 5120 * 4 <= full and S.sarathi_mx_linear_plan(*args, 0)[2] == 1
+    assert S.sarathi_mx_linear_plan(*args, 2 * 200 * 5120 * 4)[2] <= 2
+    assert S.sarathi_mx_linear_plan(S.BF16, S.LINEAR_SWIGLU, S.MX_E2M1, 200, 512, 13824, full)[2] == 1
+    assert S.sarathi_mx_linear_plan(S.BF16, S.LINEAR_PLAIN, S.MX_E4M3, 1, 64, 64, 0) == (32, 32, 1)
+    one = ct.c_int()
+    lib = S.lib()
+    assert lib.sarathi_mx_linear_plan(*args, 0, None, ct.byref(one), ct.byref(one)) == S.EINVAL
+    for kw, code in BAD_LINEAR[:11]:
+        a = {**LINEAR, **kw}
+        assert lib.sarathi_mx_linear_plan(a["dtype"], a["kind"], a["a_format"], a["M"], a["N"], a["K"], 0, ct.byref(one),
+                                          ct.byref(one), ct.byref(one)) == (code if "resid" not in kw else S.OK)
+
+
 # ------------------------------------------------------------------ pins of the oracle
 
 def test_grids():
