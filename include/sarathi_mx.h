@@ -80,10 +80,10 @@ int sarathi_mx_dequantize(int format, int rows, int cols, const void* operand, s
  * [cols] of dtype (stream_dtype F32 with either, BF16 with BF16).  delta may be
  * NULL (h = x) and h_out may be NULL (not wanted) or x itself (ld_h == ld_x);
  * otherwise h_out overlaps neither x nor delta.  The sum is taken in fp32 and
- * rounded once to h_out; the norm takes the fp32 sum, its own arithmetic in
- * fp64, and is rounded once to fp32 before its codes.  cols is at most 24576.
- * A row that holds an infinity or NaN, or whose h^2 sum to more than fp64 holds
- * (none in fp32), becomes NaN where the formula does.
+ * rounded once to h_out; the norm takes the fp32 sum in
+ * more than fp32's precision: an element's code is that of its value to about
+ * 2^-45 of it.  cols is at most 24576.
+ * A row that holds an infinity or NaN becomes NaN where the formula does.
  * Errors: as sarathi_mx_quantize; EINVAL (eps not > 0, overlaps), EUNSUPPORTED
  * (cols, stream_dtype BF16 with dtype F32).
  */

@@ -1,4 +1,11 @@
-// Products of microscaled operands with the epilogues of the linear ops.
+// Products of microscaled operands with the epilogues of the linear ops:
+//   out = epilogue(sum_b 2^(sa_b + sw_b) sum_{k in block b} a_k w_k),
+// on the matrix cores' scaled instruction, which takes both operands' codes and block scales.  Two kernels.  Up to 64 (128)
+// rows the weights stream from memory into registers as fragments: bound by that stream (4 rows of 15360 x 5120: 10.3 us,
+// 4.1 TB/s, where 2 of the 10 are the launch).  More rows run as tiles fed through LDS: bound by the matrix cores and the
+// power that they draw (probes of the loop alone reach 6.0 PFLOP/s of e2m1 on random codes, 8.9 on constant ones; 4096 rows
+// of 27648 x 5120 with SwiGLU run at 4.0 to 4.1), and for a few hundred rows by the chain of a stage (barrier, LDS reads,
+// products) on one tile per CU.
 #include <algorithm>
 #include <cmath>
 
@@ -560,7 +567,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxLinearArgs p, int splits
 // Most that split columns can use: at most 256 tiles run, of 64 K output elements at most; eight splits.
 constexpr int MX_MAX_SPLITS = 8;
 size_t mx_linear_parts(int M, int N) {
-  if (M <= MX_ROWS) return 0;
+  if (M <= 2 * MX_ROWS) return 0;
   return std::min((size_t)MX_MAX_SPLITS * M * N, (size_t)256 * 65536);
 }
 
@@ -644,10 +651,10 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
   const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
   const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
   // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
-  // e2m1: 9.6 us, 14 there).  Not where there are few W tiles and many columns, which the other kernel can split
-  // (STREAMFIG).
+  // e2m1: 9.6 us, 14 there), but not where it can split many columns of few W tiles (128 rows of 5120 x 13824: e2m1 24.5 us
+  // streamed, 19.9 split; e4m3 35.2 and 22.9).
   const bool few = w_tiles <= 256, split = few && a.quads > 32 && a.parts && !glu && a.N % 4 == 0;
-  if (x_tiles == 1 || (x_tiles == 2 && !split) || (x_tiles <= 4 && few && !split)) {
+  if (x_tiles <= 2 || (x_tiles <= 4 && few && !split)) {
     switch (x_tiles) {
       case 1:
         if (glu) return run_stream<FMT, EXACT, 8, 2, 1>(a, s, plan);

@@ -113,7 +113,7 @@ def test_linear_refuses(kw, code):
 
 
 def test_linear_plan():
-    assert S.sarathi_mx_linear_scratch_bytes(32, 1 << 20) == 0
+    assert S.sarathi_mx_linear_scratch_bytes(64, 1 << 20) == 0
     full = S.sarathi_mx_linear_scratch_bytes(200, 5120)
     assert 0 < full <= 8 * 200 * 5120 * 4 and S.sarathi_mx_linear_scratch_bytes(4096, 28000) <= 64 << 20
     args = (S.BF16, S.LINEAR_PLAIN, S.MX_E2M1, 200, 5120, 13824)
