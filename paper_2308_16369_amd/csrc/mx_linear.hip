@@ -282,7 +282,6 @@ __device__ __forceinline__ void pin_regs(V (&r)[N]) {      // no use of r moves 
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(r[i]));
 }
-constexpr int MX_MAX_STAGES = 12;
 template <int FMT, int WGN, int WGM, int FN, int FM>
 struct MxTile {
   static constexpr int XU = FMT == E2M1 ? 1 : 2;
@@ -297,7 +296,10 @@ struct MxTile {
   static constexpr int PAD = 36;                                             // floats of a row of the epilogue's tile
   static constexpr int OUT = NW * 32 * PAD * 4;
   static constexpr int most(int a, int b) { return a < b ? a : b; }
-  static constexpr int NS = most(most((160 * 1024 - SR * SCALES - OUT) / STAGE, (56 - 3 * SPER) / PER), most(MX_MAX_STAGES, SR * SPQ));
+  // Whole quads, so that a stage's place goes by its place in the quad (4 or 8; with 6 the e2m1 256 x 256 tiles took 280 us
+  // where four take 257, the e4m3 256 x 128 ones 447 and 416).
+  static constexpr int FIT = most(most((160 * 1024 - SR * SCALES - OUT) / STAGE, (56 - 3 * SPER) / PER), most(8, SR * SPQ));
+  static constexpr int NS = FIT / 4 * 4;
   static constexpr int LDS = SR * SCALES + NS * STAGE + OUT;
   // requests of scales with the n stages before stage j of a quad (one with each quad's first, before the stage's own)
   static constexpr int scale_requests(int j, int n) { return j > 0 ? (n >= j ? (n - j) / SPQ + 1 : 0) : n / SPQ; }
@@ -611,16 +613,16 @@ static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s, MxLinearPlan*
 }
 
 // The tiles of the second kernel (W tiles by x tiles) and what 64 columns of one cost with every CU busy, in us (from 4096
-// rows of 13824 x 5120, a round of one tile per CU: e2m1 12.1, 15.5, 27.5, 28.8, 32.2, 40 us in the order below, e4m3 14.5,
-// 23.4, 33, 39.6 and 53.7, with exact sums 27, 37, 55 and 98; 2.5 of them the output's).  0: not built, another tile is
+// rows of 13824 x 5120, a round of one tile per CU: e2m1 12.1, 15.5, 27, 28, 31, 37 us in the order below, e4m3 14.5, 20.5,
+// 31, 39.6 and 53.7, with exact sums 27, 35, 54 and 98; 2.5 of them the output's).  0: not built, another tile is
 // faster everywhere (the split of an x fragment for exact sums is shared by FN W tiles).  Where tiles leave CUs idle, the
 // columns are split: shorter tiles, but the partial sums are written and read back, and a launch of their own joins them.
 struct TileCost {
   int tn, tm;
   float e2m1, e4m3, exact;
 };
-constexpr TileCost kTiles[] = {{4, 2, 0.120f, 0.150f, 0.306f}, {4, 4, 0.160f, 0.260f, 0.430f}, {8, 4, 0.31f, 0.385f, 0.66f},
-                               {4, 10, 0.33f, 0.465f, 0},      {8, 6, 0.37f, 0, 0},            {8, 8, 0.47f, 0.64f, 1.19f}};
+constexpr TileCost kTiles[] = {{4, 2, 0.120f, 0.150f, 0.306f}, {4, 4, 0.160f, 0.225f, 0.40f}, {8, 4, 0.305f, 0.36f, 0.64f},
+                               {4, 10, 0.32f, 0.465f, 0},      {8, 6, 0.355f, 0, 0},          {8, 8, 0.43f, 0.64f, 1.19f}};
 
 struct TilePick {
   int tile, splits;
