@@ -82,10 +82,10 @@ int sarathi_mx_dequantize(int format, int rows, int cols, const void* operand, s
  * otherwise h_out overlaps neither x nor delta.  The sum is taken in fp32 and
  * rounded once to h_out; the norm takes the fp32 sum in
  * more than fp32's precision: an element's code is that of its value to about
- * 2^-45 of it.  cols is at most 24576.
+ * 2^-45 of it.  cols is at most 24576, rows at most 2^24 - 256.
  * A row that holds an infinity or NaN becomes NaN where the formula does.
  * Errors: as sarathi_mx_quantize; EINVAL (eps not > 0, overlaps), EUNSUPPORTED
- * (cols, stream_dtype BF16 with dtype F32).
+ * (rows, cols, stream_dtype BF16 with dtype F32).
  */
 int sarathi_mx_norm(int stream_dtype, int dtype, int format, int rows, int cols, float eps, const void* x, size_t ld_x,
                     const void* delta, size_t ld_delta, const void* gain, void* h_out, size_t ld_h, void* operand,
@@ -107,9 +107,11 @@ int sarathi_mx_norm(int stream_dtype, int dtype, int format, int rows, int cols,
  * product, against the half step of 2^-4 that its code already has).
  * `scratch`: as for sarathi_linear, for partial sums of split columns; with
  * NULL or less than sarathi_mx_linear_scratch_bytes(M, N) fewer splits are used.
+ * Calls that may run at once have scratch of their own.
  * Results do not depend on the order in which work runs.
- * Errors: EINVAL (NULL, sizes, kind, alignment), EUNSUPPORTED (dtype, a_format,
- * K not a multiple of 8, more than 2^24 - 1 tiles), EHIP.
+ * Errors: EINVAL (NULL, sizes, kind, alignment, overlaps), EUNSUPPORTED (dtype, a_format,
+ * K not a multiple of 8, more than 2^24 - 1 tiles of either operand or of
+ * 32 x 32 outputs, N of more than 2^23 - 1 tiles of 32), EHIP.
  */
 size_t sarathi_mx_linear_scratch_bytes(int M, int N);
 /* What sarathi_mx_linear would run with scratch_bytes of scratch, as sarathi_linear_plan: *bm rows of a by *bn rows of w

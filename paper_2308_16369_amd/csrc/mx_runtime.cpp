@@ -2,6 +2,7 @@
 // enqueued) and the operators' launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "host_error.h"
@@ -12,7 +13,10 @@ using namespace sarathi;
 
 namespace {
 
-constexpr long MAX_TILES = (1l << 24) - 1;   // blocks of 256 threads in one launch
+// A launch holds fewer than 2^32 threads.
+constexpr long MAX_TILES = (1l << 24) - 1;         // blocks of 256 threads
+constexpr long MAX_W_TILES = (1l << 23) - 1;       // of 512: the product of few rows, a block per W tile
+constexpr int MAX_NORM_ROWS = (1 << 24) - 256;     // of 256: a row to a block, in groups of 256
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 size_t esize(int dtype) { return dtype == SARATHI_BF16 ? 2 : 4; }
@@ -63,6 +67,7 @@ int check_linear(int dtype, int kind, int a_format, int M, int N, int K) {
   if (K % 8) return fail(SARATHI_EUNSUPPORTED, "K %d must be a multiple of 8", K);
   if (!sizes_fit(M, K) || !sizes_fit(N, K) || (long)mx_tiles(M) * mx_tiles(N) > MAX_TILES)
     return fail(SARATHI_EUNSUPPORTED, "%d x %d x %d is more than %ld tiles", M, N, K, MAX_TILES);
+  if (mx_tiles(N) > MAX_W_TILES) return fail(SARATHI_EUNSUPPORTED, "N %d is more than %ld tiles", N, MAX_W_TILES);
   return SARATHI_OK;
 }
 
@@ -127,6 +132,7 @@ int sarathi_mx_norm(int stream_dtype, int dtype, int format, int rows, int cols,
     return fail(SARATHI_EUNSUPPORTED, "stream_dtype %d with dtype %d", stream_dtype, dtype);
   int rc = check_operand(format, rows, cols);
   if (rc) return rc;
+  if (rows > MAX_NORM_ROWS) return fail(SARATHI_EUNSUPPORTED, "rows %d above %d", rows, MAX_NORM_ROWS);
   if (cols > MX_NORM_COLS) return fail(SARATHI_EUNSUPPORTED, "cols %d above %d", cols, MX_NORM_COLS);
   if (!(eps > 0.f) || !std::isfinite(eps)) return fail(SARATHI_EINVAL, "eps must be > 0");
   const size_t ss = esize(stream_dtype), es = esize(dtype);
@@ -166,7 +172,7 @@ int sarathi_mx_linear_plan(int dtype, int kind, int a_format, int M, int N, int 
   MxLinearArgs p{};
   p.kind = kind; p.dtype = dtype; p.M = M; p.N = N; p.quads = mx_quads(K);
   p.parts = scratch_bytes >= 4 ? &dummy : nullptr;
-  p.parts_cap = scratch_bytes / 4;
+  p.parts_cap = std::min(scratch_bytes / 4, mx_linear_parts(M, N));
   MxLinearPlan pl{};
   if (launch_mx_linear(a_format, p, nullptr, &pl) != hipSuccess) return fail(SARATHI_EINVAL, "no plan for this op");
   *bm = pl.bm; *bn = pl.bn; *n_split = pl.splits;
@@ -190,6 +196,13 @@ int sarathi_mx_linear(int dtype, int kind, int a_format, int M, int N, int K, co
     return fail(SARATHI_EINVAL, "out overlaps an operand");
   if (needs_resid && (resid == out ? rs != os : overlap(out, n * os, resid, n * rs)))
     return fail(SARATHI_EINVAL, "out overlaps resid (it may be resid where their types are the same)");
+  const size_t parts = std::min(scratch_bytes / 4, mx_linear_parts(M, N));
+  if (scratch && parts) {
+    if (overlap(scratch, parts * 4, out, n * os) || overlap(scratch, parts * 4, a, na) ||
+        overlap(scratch, parts * 4, w, kind == SARATHI_LINEAR_SWIGLU ? 2 * nw : nw) ||
+        (needs_resid && overlap(scratch, parts * 4, resid, n * rs)))
+      return fail(SARATHI_EINVAL, "scratch overlaps an operand, out or resid");
+  }
   MxLinearArgs p{};
   p.kind = kind; p.dtype = dtype; p.M = M; p.N = N; p.quads = mx_quads(K);
   p.a = static_cast<const char*>(a);
@@ -201,7 +214,7 @@ int sarathi_mx_linear(int dtype, int kind, int a_format, int M, int N, int K, co
   p.out = out;
   if (scratch && aligned16(scratch)) {
     p.parts = static_cast<float*>(scratch);
-    p.parts_cap = scratch_bytes / 4;
+    p.parts_cap = parts;
   }
   const hipError_t e = launch_mx_linear(a_format, p, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? SARATHI_OK : hip_fail(e, "mx_linear");

@@ -77,7 +77,7 @@ NORM = dict(stream_dtype=S.F32, dtype=S.BF16, format=S.MX_E4M3, rows=40, cols=64
 BAD_NORM = [
     (dict(stream_dtype=2), S.EUNSUPPORTED), (dict(dtype=-1), S.EUNSUPPORTED),
     (dict(stream_dtype=S.BF16, dtype=S.F32), S.EUNSUPPORTED), (dict(format=3), S.EUNSUPPORTED), (dict(rows=0), S.EINVAL),
-    (dict(cols=0), S.EINVAL), (dict(cols=20), S.EUNSUPPORTED),
+    (dict(cols=0), S.EINVAL), (dict(cols=20), S.EUNSUPPORTED), (dict(rows=2 ** 24 - 255), S.EUNSUPPORTED),
     (dict(cols=24584, ld_x=24584, ld_delta=24584, ld_h=24584), S.EUNSUPPORTED), (dict(eps=0.0), S.EINVAL),
     (dict(eps=-1.0), S.EINVAL), (dict(eps=float("nan")), S.EINVAL), (dict(eps=float("inf")), S.EINVAL),
     (dict(x=0), S.EINVAL), (dict(x=A + 4), S.EINVAL), (dict(ld_x=32), S.EINVAL), (dict(delta=B + 2), S.EINVAL),
@@ -99,6 +99,9 @@ BAD_LINEAR = [
     (dict(dtype=2), S.EUNSUPPORTED), (dict(kind=-1), S.EINVAL), (dict(kind=5), S.EINVAL), (dict(a_format=2), S.EUNSUPPORTED),
     (dict(M=0), S.EINVAL), (dict(N=0), S.EINVAL), (dict(K=0), S.EINVAL), (dict(K=-8), S.EINVAL), (dict(K=36), S.EUNSUPPORTED),
     (dict(M=2 ** 31 - 1, N=2 ** 31 - 1), S.EUNSUPPORTED), (dict(M=2 ** 31 - 1, K=2 ** 20), S.EUNSUPPORTED),
+    (dict(M=1, N=2 ** 28 - 31), S.EUNSUPPORTED), (dict(scratch=D, scratch_bytes=1 << 20, M=200), S.EINVAL),
+    (dict(scratch=A, scratch_bytes=1 << 20, M=200), S.EINVAL), (dict(scratch=B, scratch_bytes=1 << 20, M=200), S.EINVAL),
+    (dict(scratch=C, scratch_bytes=1 << 20, M=200), S.EINVAL),
     (dict(a=0), S.EINVAL), (dict(w=0), S.EINVAL), (dict(out=0), S.EINVAL), (dict(resid=0), S.EINVAL),
     (dict(kind=S.LINEAR_RESID, resid=0), S.EINVAL), (dict(a=A + 8), S.EINVAL), (dict(w=B + 4), S.EINVAL),
     (dict(out=D + 8), S.EINVAL), (dict(resid=C + 4), S.EINVAL), (dict(out=A), S.EINVAL), (dict(out=B), S.EINVAL),
