@@ -42,8 +42,9 @@ __device__ __forceinline__ floatx16 mx_mfma(const u32x4& w, uint32_t ws, const u
       i32x8 lo;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t u = (uint32_t)b[i], t = u & 0x40404040u, m = (t << 1) - (t >> 6);   // 0x7f in the bytes of the upper half
-        b[i] = (int)(u & (m | 0x80808080u));
+        // 0xff in the bytes of the upper half: selectors 8 .. 11 repeat the top bits of bytes 1 and 3 of either operand
+        const uint32_t u = (uint32_t)b[i], m = __builtin_amdgcn_perm(u << 9, u << 1, 0x090b080au);
+        b[i] = (int)(u & m);
         lo[i] = (int)(u & ~m);
       }
       c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 0, S, (int)ws, S, (int)xs);
@@ -64,12 +65,18 @@ __device__ __forceinline__ float swiglu_f(float z, float u) { return z * __built
 __device__ __forceinline__ bool adds_resid(const MxLinearArgs& p) {
   return p.kind == SARATHI_LINEAR_RESID || p.kind == SARATHI_LINEAR_RESID_F32IN;
 }
-// The residual at columns n .. n + 3 of row m (N a multiple of 4).
-__device__ __forceinline__ float4 load_resid4(const MxLinearArgs& p, int m, int n) {
+// The residual at columns n .. n + 3 of row m (N a multiple of 4), as it lies in memory, and its values.
+__device__ __forceinline__ bool resid_f32(const MxLinearArgs& p) {
+  return p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN;
+}
+__device__ __forceinline__ uint4 load_resid4(const MxLinearArgs& p, int m, int n) {
   const size_t at = (size_t)m * p.N + n;
-  if (p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN)
-    return *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.resid) + at);
+  if (resid_f32(p)) return *reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.resid) + at);
   const uint2 r = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p.resid) + at);
+  return make_uint4(r.x, r.y, 0, 0);
+}
+__device__ __forceinline__ float4 resid4(const MxLinearArgs& p, const uint4& r) {
+  if (resid_f32(p)) return __builtin_bit_cast(float4, r);
   return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
                      __uint_as_float(r.y & 0xffff0000u));
 }
@@ -89,7 +96,7 @@ __device__ __forceinline__ void put_any(const MxLinearArgs& p, int m, int n, flo
     float z = v.x;
     v = make_float4(v.y, v.z, v.w, v.x);
     if (adds_resid(p))
-      z += p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN
+      z += resid_f32(p)
                ? reinterpret_cast<const float*>(p.resid)[at]
                : bf2f(reinterpret_cast<const bf16*>(p.resid)[at]);
     if (p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID) reinterpret_cast<float*>(p.out)[at] = z;
@@ -103,7 +110,7 @@ __device__ __forceinline__ float4 add4(const float4& a, const float4& b) {
 __device__ __forceinline__ void mx_store4(const MxLinearArgs& p, int m, int n, const float4& v) {
   if (m >= p.M || n >= p.N) return;
   if (p.N % 4) put_any(p, m, n, v);
-  else put4(p, m, n, adds_resid(p) ? add4(v, load_resid4(p, m, n)) : v);
+  else put4(p, m, n, adds_resid(p) ? add4(v, resid4(p, load_resid4(p, m, n))) : v);
 }
 
 // W tile t of a product's columns (SwiGLU: even ones are tiles of the gate, odd ones those of up): bytes from the first
@@ -510,6 +517,16 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
     const int m0 = (at.tm * TM + wm * FM) * 32 + r0, n0 = (at.tn * WGN + wn) * FO * W + c0;
     const uint32_t put_at = out + ((le & 31) * T::PAD + 4 * (le >> 5)) * 4, get_at = out + (r0 * T::PAD + c0) * 4;
     const bool add = !GLU && splits == 1 && adds_resid(p) && p.N % 4 == 0;
+    // The piece's residual, requested a piece ahead (1955 rows of 6656 x 6656, fp32 out, e2m1: 53.5 us, 60 without); the
+    // 256 x 256 tiles of e4m3 rows with single products have no registers left for it.
+    constexpr bool AHEAD = PIECES > 1 && (FMT == E2M1 || EXACT || PIECES < 8);
+    uint4 raw[ROWS];
+    auto fetch = [&](int piece) {
+      const int m = m0 + piece / FO * 32, n = min(n0 + piece % FO * W, p.N - 4);
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) raw[i] = load_resid4(p, min(m + i * PR, p.M - 1), n);
+    };
+    if (AHEAD && add) fetch(0);
 #pragma unroll 1
     for (int piece = 0; piece < PIECES; ++piece) {
       static_for<0, PIECES>([&](auto ic) {
@@ -528,11 +545,10 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
       pin_regs(v);
       const int m = m0 + piece / FO * 32, n = n0 + piece % FO * W;
       if (add) {
-        float4 res[ROWS];
+        if (!AHEAD) fetch(piece);
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) res[i] = load_resid4(p, min(m + i * PR, p.M - 1), min(n, p.N - 4));
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) v[i] = __builtin_bit_cast(u32x4, add4(__builtin_bit_cast(float4, v[i]), res[i]));
+        for (int i = 0; i < ROWS; ++i) v[i] = __builtin_bit_cast(u32x4, add4(__builtin_bit_cast(float4, v[i]), resid4(p, raw[i])));
+        if (AHEAD && piece + 1 < PIECES) fetch(piece + 1);
       } else if (!GLU && splits == 1 && p.kind == SARATHI_LINEAR_GELU) {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
@@ -614,15 +630,15 @@ static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s, MxLinearPlan*
 
 // The tiles of the second kernel (W tiles by x tiles) and what 64 columns of one cost with every CU busy, in us (from 4096
 // rows of 13824 x 5120, a round of one tile per CU: e2m1 12.1, 15.5, 27, 28, 31, 37 us in the order below, e4m3 14.5, 20.5,
-// 31, 39.6 and 53.7, with exact sums 27, 35, 54 and 98; 2.5 of them the output's).  0: not built, another tile is
+// 31, 39.6 and 53.7, with exact sums 22, 33, 52 and 97; 2.5 of them the output's).  0: not built, another tile is
 // faster everywhere (the split of an x fragment for exact sums is shared by FN W tiles).  Where tiles leave CUs idle, the
 // columns are split: shorter tiles, but the partial sums are written and read back, and a launch of their own joins them.
 struct TileCost {
   int tn, tm;
   float e2m1, e4m3, exact;
 };
-constexpr TileCost kTiles[] = {{4, 2, 0.120f, 0.150f, 0.306f}, {4, 4, 0.160f, 0.225f, 0.40f}, {8, 4, 0.305f, 0.36f, 0.64f},
-                               {4, 10, 0.32f, 0.465f, 0},      {8, 6, 0.355f, 0, 0},          {8, 8, 0.43f, 0.64f, 1.19f}};
+constexpr TileCost kTiles[] = {{4, 2, 0.120f, 0.150f, 0.245f}, {4, 4, 0.160f, 0.225f, 0.385f}, {8, 4, 0.305f, 0.36f, 0.62f},
+                               {4, 10, 0.32f, 0.465f, 0},      {8, 6, 0.355f, 0, 0},          {8, 8, 0.43f, 0.64f, 1.18f}};
 
 struct TilePick {
   int tile, splits;

@@ -270,9 +270,10 @@ PICKS = [
     ("e4m3", "bf16", "swiglu", 2100, 7000, 520, 256, 256, 0),
     ("e4m3", "f32", "plain", 130, 100, 264, 64, 128, 0), ("e4m3", "bf16", "resid", 258, 6661, 264, 128, 128, 0),
     ("e4m3", "f32", "gelu", 258, 14000, 264, 128, 256, 0), ("e4m3", "bf16", "resid", 1600, 5000, 776, 256, 256, 0),
-    ("e4m3", "f32", "plain", 130, 100, 2560, 64, 128, 1), ("e4m3", "bf16", "resid", 70, 3500, 8712, 128, 128, 1),
+    ("e4m3", "f32", "plain", 130, 100, 2560, 64, 128, 1), ("e4m3", "bf16", "resid", 258, 3500, 8712, 128, 128, 1),
     ("e4m3", "f32", "resid_f32in", 70, 8200, 8712, 128, 256, 1), ("e4m3", "f32", "swiglu", 70, 10000, 264, 128, 128, 0),
     ("e4m3", "f32", "swiglu", 130, 10000, 264, 128, 256, 0), ("e4m3", "f32", "swiglu", 2100, 7000, 264, 256, 256, 0),
+    ("e4m3", "bf16", "resid", 700, 6660, 8712, 256, 256, 1), ("e4m3", "bf16", "resid", 258, 6660, 8712, 128, 256, 1),
 ]
 
 
