@@ -17,6 +17,8 @@ inline int mx_tiles(int rows) { return (int)(((long)rows + MX_ROWS - 1) / MX_ROW
 inline int mx_quads(int cols) { return (int)(((long)cols + MX_COLS - 1) / MX_COLS); }
 // codes of one row tile: 32 rows of 128 (e2m1) or 256 bytes per 256 columns
 inline size_t mx_tile_bytes(int format, int cols) { return (size_t)mx_quads(cols) * MX_ROWS * (format ? 256 : 128); }
+// columns of partial sums: rows of whole float4
+__host__ __device__ inline size_t mx_part_cols(int N) { return ((size_t)N + 3) & ~(size_t)3; }
 inline size_t mx_scale_offset(int format, int rows, int cols) { return mx_tiles(rows) * mx_tile_bytes(format, cols); }
 inline size_t mx_bytes(int format, int rows, int cols) {
   return mx_scale_offset(format, rows, cols) + (size_t)mx_tiles(rows) * mx_quads(cols) * 256;
@@ -54,7 +56,7 @@ struct MxLinearArgs {
   size_t up;               // SwiGLU: bytes from gate to up, codes and scales alike
   const void* resid;
   void* out;
-  float* parts;            // [split][M][N], or NULL
+  float* parts;            // [split][M][mx_part_cols(N)], or NULL
   size_t parts_cap;        // floats
 };
 struct MxLinearPlan {

@@ -65,31 +65,38 @@ __device__ __forceinline__ float swiglu_f(float z, float u) { return z * __built
 __device__ __forceinline__ bool adds_resid(const MxLinearArgs& p) {
   return p.kind == SARATHI_LINEAR_RESID || p.kind == SARATHI_LINEAR_RESID_F32IN;
 }
-// The residual at columns n .. n + 3 of row m (N a multiple of 4), as it lies in memory, and its values.
+// Four columns of a row of any N: the rows need not be aligned, the memory instructions take them so (one element at a
+// time, 1956 rows of 4181 x 120 onto fp32 took 63 us).
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+// The residual at columns n .. n + 3 <= N - 1 of row m, as it lies in memory, and its values.
 __device__ __forceinline__ bool resid_f32(const MxLinearArgs& p) {
   return p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN;
 }
 __device__ __forceinline__ uint4 load_resid4(const MxLinearArgs& p, int m, int n) {
   const size_t at = (size_t)m * p.N + n;
-  if (resid_f32(p)) return *reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.resid) + at);
-  const uint2 r = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p.resid) + at);
-  return make_uint4(r.x, r.y, 0, 0);
+  if (resid_f32(p)) {
+    const u32x4_any r = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const float*>(p.resid) + at);
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  }
+  const u32x2_any r = *reinterpret_cast<const u32x2_any*>(reinterpret_cast<const bf16*>(p.resid) + at);
+  return make_uint4(r[0], r[1], 0, 0);
 }
 __device__ __forceinline__ float4 resid4(const MxLinearArgs& p, const uint4& r) {
   if (resid_f32(p)) return __builtin_bit_cast(float4, r);
   return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
                      __uint_as_float(r.y & 0xffff0000u));
 }
-// Columns n .. n + 3 of row m of the output, rounded to its type (N a multiple of 4).
+// Columns n .. n + 3 <= N - 1 of row m of the output, rounded to its type.
 __device__ __forceinline__ void put4(const MxLinearArgs& p, int m, int n, const float4& v) {
   const size_t at = (size_t)m * p.N + n;
   if (p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID)
-    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = v;
+    *reinterpret_cast<u32x4_any*>(reinterpret_cast<float*>(p.out) + at) = __builtin_bit_cast(u32x4, v);
   else
-    *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(p.out) + at) = make_uint2(pk_bf16(v.x, v.y), pk_bf16(v.z, v.w));
+    *reinterpret_cast<u32x2_any*>(reinterpret_cast<bf16*>(p.out) + at) = u32x2_any{pk_bf16(v.x, v.y), pk_bf16(v.z, v.w)};
 }
-// The same for any N, with the residual added.
-__device__ __forceinline__ void put_any(const MxLinearArgs& p, int m, int n, float4 v) {
+// The last columns of a row, fewer than four, with the residual added.
+__device__ __forceinline__ void put_last(const MxLinearArgs& p, int m, int n, float4 v) {
 #pragma unroll 1
   for (int i = 0; i < 4 && n + i < p.N; ++i) {
     const size_t at = (size_t)m * p.N + n + i;
@@ -109,7 +116,7 @@ __device__ __forceinline__ float4 add4(const float4& a, const float4& b) {
 // One such piece from sums v.
 __device__ __forceinline__ void mx_store4(const MxLinearArgs& p, int m, int n, const float4& v) {
   if (m >= p.M || n >= p.N) return;
-  if (p.N % 4) put_any(p, m, n, v);
+  if (n + 4 > p.N) put_last(p, m, n, v);
   else put4(p, m, n, adds_resid(p) ? add4(v, resid4(p, load_resid4(p, m, n))) : v);
 }
 
@@ -516,7 +523,7 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
     const int r0 = le / (W / 4), c0 = le % (W / 4) * 4;
     const int m0 = (at.tm * TM + wm * FM) * 32 + r0, n0 = (at.tn * WGN + wn) * FO * W + c0;
     const uint32_t put_at = out + ((le & 31) * T::PAD + 4 * (le >> 5)) * 4, get_at = out + (r0 * T::PAD + c0) * 4;
-    const bool add = !GLU && splits == 1 && adds_resid(p) && p.N % 4 == 0;
+    const bool add = !GLU && splits == 1 && adds_resid(p) && p.N >= 4;
     // The piece's residual, requested a piece ahead (1955 rows of 6656 x 6656, fp32 out, e2m1: 53.5 us, 60 without); the
     // 256 x 256 tiles of e4m3 rows with single products have no registers left for it.
     constexpr bool AHEAD = PIECES > 1 && (FMT == E2M1 || EXACT || PIECES < 8);
@@ -547,7 +554,10 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
       if (add) {
         if (!AHEAD) fetch(piece);
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) v[i] = __builtin_bit_cast(u32x4, add4(__builtin_bit_cast(float4, v[i]), resid4(p, raw[i])));
+        for (int i = 0; i < ROWS; ++i) {
+          const u32x4 y = __builtin_bit_cast(u32x4, add4(__builtin_bit_cast(float4, v[i]), resid4(p, raw[i])));
+          if (n + 4 <= p.N) v[i] = y;
+        }
         if (AHEAD && piece + 1 < PIECES) fetch(piece + 1);
       } else if (!GLU && splits == 1 && p.kind == SARATHI_LINEAR_GELU) {
 #pragma unroll
@@ -560,8 +570,8 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
         const int row = m + i * PR;
         if (row >= p.M || n >= p.N) continue;
         const float4 y = __builtin_bit_cast(float4, v[i]);
-        if (!GLU && splits > 1) *reinterpret_cast<float4*>(p.parts + ((size_t)at.split * p.M + row) * p.N + n) = y;
-        else if (p.N % 4) put_any(p, row, n, y);
+        if (!GLU && splits > 1) *reinterpret_cast<float4*>(p.parts + ((size_t)at.split * p.M + row) * mx_part_cols(p.N) + n) = y;
+        else if (n + 4 > p.N) put_last(p, row, n, y);
         else put4(p, row, n, y);
       }
     }
@@ -571,7 +581,8 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
 
 // The partial sums of `splits` shares of the columns, added in order; four columns to a thread.
 __global__ __launch_bounds__(256) void mx_join_kernel(MxLinearArgs p, int splits) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, size = (size_t)p.M * p.N;
+  const size_t cols = mx_part_cols(p.N);
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, size = (size_t)p.M * cols;
   if (i * 4 >= size) return;
   float4 v = reinterpret_cast<const float4*>(p.parts)[i];
   for (int s = 1; s < splits; ++s) {
@@ -579,14 +590,14 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxLinearArgs p, int splits
     v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
   }
   if (p.kind == SARATHI_LINEAR_GELU) v = make_float4(gelu_f(v.x), gelu_f(v.y), gelu_f(v.z), gelu_f(v.w));
-  mx_store4(p, (int)(i * 4 / p.N), (int)(i * 4 % p.N), v);
+  mx_store4(p, (int)(i * 4 / cols), (int)(i * 4 % cols), v);
 }
 
 // Most that split columns can use: at most 256 tiles run, of 64 K output elements at most; eight splits.
 constexpr int MX_MAX_SPLITS = 8;
 size_t mx_linear_parts(int M, int N) {
   if (M <= 2 * MX_ROWS) return 0;
-  return std::min((size_t)MX_MAX_SPLITS * M * N, (size_t)256 * 65536);
+  return std::min((size_t)MX_MAX_SPLITS * M * mx_part_cols(N), (size_t)256 * 65536);
 }
 
 template <int FMT, bool EXACT, bool GLU, int WGN, int WGM, int FN, int FM>
@@ -603,7 +614,7 @@ static hipError_t run_tile_as(const MxLinearArgs& a, int splits, hipStream_t s) 
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * T::NW), T::LDS, s, a, tiles_m, tiles_n, splits);
   e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
-  hipLaunchKernelGGL(mx_join_kernel, dim3((unsigned)(((size_t)a.M * a.N / 4 + 255) / 256)), dim3(256), 0, s, a, splits);
+  hipLaunchKernelGGL(mx_join_kernel, dim3((unsigned)(((size_t)a.M * mx_part_cols(a.N) / 4 + 255) / 256)), dim3(256), 0, s, a, splits);
   return hipGetLastError();
 }
 
@@ -646,9 +657,9 @@ struct TilePick {
 static TilePick pick_tile(const MxLinearArgs& a, int w_tiles, int x_tiles, int format, bool exact) {
   TilePick best{0, 1};
   float least = INFINITY;
-  const size_t size = (size_t)a.M * a.N;
+  const size_t size = (size_t)a.M * mx_part_cols(a.N);
   // (partial sums of SwiGLU would be two for each output, and its W tiles are many)
-  const bool can_split = a.parts && a.kind != SARATHI_LINEAR_SWIGLU && a.N % 4 == 0;
+  const bool can_split = a.parts && a.kind != SARATHI_LINEAR_SWIGLU;
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const TileCost& t = kTiles[i];
     const float cost = exact ? t.exact : format == E2M1 ? t.e2m1 : t.e4m3;
@@ -671,7 +682,7 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
   // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
   // e2m1: 9.6 us, 14 there), but not where it can split many columns of few W tiles (128 rows of 5120 x 13824: e2m1 24.5 us
   // streamed, 19.9 split; e4m3 35.2 and 22.9).
-  const bool few = w_tiles <= 256, split = few && a.quads > 32 && a.parts && !glu && a.N % 4 == 0;
+  const bool few = w_tiles <= 256, split = few && a.quads > 32 && a.parts && !glu;
   if (x_tiles <= 2 || (x_tiles <= 4 && few && !split)) {
     switch (x_tiles) {
       case 1:
