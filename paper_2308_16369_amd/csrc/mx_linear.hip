@@ -680,9 +680,9 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
   const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
   const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
   // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
-  // e2m1: 9.6 us, 14 there), but not where it can split many columns of few W tiles (128 rows of 5120 x 13824: e2m1 24.5 us
-  // streamed, 19.9 split; e4m3 35.2 and 22.9).
-  const bool few = w_tiles <= 256, split = few && a.quads > 32 && a.parts && !glu;
+  // e2m1: 9.6 us, 14 there), but not where it can split many columns of few W tiles (128 rows of 2600 x 13824: e2m1 20.7 us
+  // streamed, 17.8 split; e4m3 31.2 and 18.3; 96 rows of 5120 x 8704: e2m1 13.0 and 17.0, e4m3 17.9 and 17.8).
+  const bool few = w_tiles <= 256, split = few && a.quads * (long)x_tiles > (FMT == E2M1 ? 170 : 110) && a.parts && !glu;
   if (x_tiles <= 2 || (x_tiles <= 4 && few && !split)) {
     switch (x_tiles) {
       case 1:

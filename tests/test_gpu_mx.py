@@ -257,8 +257,8 @@ PICKS = [
     ("e2m1", "bf16", "plain", 40, 100, 264, 64, 32, 0), ("e2m1", "bf16", "plain", 130, 100, 264, 64, 128, 0),
     ("e2m1", "bf16", "gelu", 258, 6660, 264, 128, 128, 0), ("e2m1", "f32", "plain", 258, 14000, 264, 128, 256, 0),
     ("e2m1", "bf16", "resid_f32in", 1600, 5001, 264, 320, 128, 0), ("e2m1", "bf16", "resid", 1300, 6660, 264, 192, 256, 0),
-    ("e2m1", "bf16", "plain", 2100, 14000, 520, 256, 256, 0), ("e2m1", "bf16", "gelu", 70, 100, 8712, 64, 128, 1),
-    ("e2m1", "bf16", "resid", 130, 5000, 8712, 64, 128, 1), ("e2m1", "f32", "resid_f32in", 70, 3500, 12808, 128, 128, 1),
+    ("e2m1", "bf16", "plain", 2100, 14000, 520, 256, 256, 0), ("e2m1", "bf16", "gelu", 70, 100, 14600, 64, 128, 1),
+    ("e2m1", "bf16", "resid", 130, 5000, 8712, 64, 128, 1), ("e2m1", "f32", "resid_f32in", 70, 3500, 14600, 128, 128, 1),
     ("e2m1", "bf16", "swiglu", 130, 100, 264, 64, 128, 0), ("e2m1", "bf16", "swiglu", 70, 10000, 264, 128, 128, 0),
     ("e2m1", "bf16", "swiglu", 130, 10000, 264, 128, 256, 0), ("e2m1", "bf16", "swiglu", 258, 14000, 264, 320, 128, 0),
     ("e2m1", "f32", "swiglu", 400, 10000, 264, 192, 256, 0), ("e2m1", "bf16", "swiglu", 2100, 7001, 776, 256, 256, 0),
