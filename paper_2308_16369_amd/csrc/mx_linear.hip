@@ -4,7 +4,7 @@
 // rows the weights stream from memory into registers as fragments: bound by that stream (4 rows of 15360 x 5120: 10.3 us,
 // 4.1 TB/s, where 2 of the 10 are the launch).  More rows run as tiles fed through LDS: bound by the matrix cores and the
 // power that they draw (probes of the loop alone reach 6.0 PFLOP/s of e2m1 on random codes, 8.9 on constant ones; 4096 rows
-// of 27648 x 5120 with SwiGLU run at 4.2, 273 us), and for a few hundred rows by the chain of a stage (barrier, LDS reads,
+// of 27648 x 5120 with SwiGLU run at 4.1 to 4.2, 273 to 285 us), and for a few hundred rows by the chain of a stage (barrier, LDS reads,
 // products) on one tile per CU.
 #include <algorithm>
 #include <cmath>

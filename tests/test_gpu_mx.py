@@ -274,6 +274,7 @@ PICKS = [
     ("e4m3", "f32", "resid_f32in", 70, 8200, 8712, 128, 256, 1), ("e4m3", "f32", "swiglu", 70, 10000, 264, 128, 128, 0),
     ("e4m3", "f32", "swiglu", 130, 10000, 264, 128, 256, 0), ("e4m3", "f32", "swiglu", 2100, 7000, 264, 256, 256, 0),
     ("e2m1", "bf16", "plain", 170, 1349, 8656, 64, 128, 1), ("e2m1", "bf16", "resid_f32in", 300, 1350, 8712, 64, 128, 1),
+    ("e4m3", "bf16", "resid_f32in", 130, 3, 264, 64, 128, 0), ("e2m1", "bf16", "resid", 300, 1, 264, 64, 128, 0),
     ("e4m3", "f32", "resid", 130, 2, 8712, 64, 128, 1), ("e4m3", "bf16", "gelu", 500, 1283, 8712, 128, 128, 1),
     ("e4m3", "bf16", "resid", 1300, 6657, 264, 256, 256, 0), ("e4m3", "bf16", "resid_f32in", 1500, 9999, 776, 256, 256, 0),
     ("e4m3", "bf16", "resid", 700, 6660, 8712, 256, 256, 1), ("e4m3", "bf16", "resid", 258, 6660, 8712, 128, 256, 1),
