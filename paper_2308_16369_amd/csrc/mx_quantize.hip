@@ -182,10 +182,13 @@ hipError_t launch_mx_dequantize(int dtype, int format, const MxQuantArgs& a, hip
 
 // ------------------------------------------------------------------ norm
 // One row per block, read once and kept in registers (eight elements to a lane,
-// NC times).  Squares are added in fp64; h r g is made of h g with its remainder
-// and of r in two parts, 45 bits, and goes to fp32 rounded to odd where a code's
-// border may be near, so that the code is that of the 45 bits.  (Plain fp32
-// products and roundings put one element in a million on a border's other side.)
+// NC times).  Squares are added in fp64.  An element's fp32 value y = h r g (h = x +
+// delta, r = 1 / sqrt(mean + eps)) carries four roundings, 2^-22 of it: up to four
+// units in the last place.  Every border of two codes or scales has its low 19 bits
+// zero, so one element in 60000 lies within four units of one; those are taken again
+// in fp64, from x and delta as they are, and rounded to odd, so that a code is that of
+// the value in 64 bits.  (Without it one element in a million takes a border's other
+// side.)
 // Bound by the rows, x and delta read, h and e4m3 codes written: 2048 x 12288 of
 // bf16, 177 MB, in 47 us from memory (3.7 TB/s), 36 over and over (4.9 TB/s).
 //
@@ -198,23 +201,29 @@ template <typename T> struct Raw8 {   // eight elements as they lie in memory
 #pragma unroll
     for (int i = 0; i < 8 / Vec16<T>::N; ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
   }
-  __device__ __forceinline__ void unpack(float* v) const {
+  __device__ __forceinline__ float at(int e) const {
+    const uint4& w = u[e / Vec16<T>::N];
+    const int i = e % Vec16<T>::N / (sizeof(T) == 2 ? 2 : 1);
+    const uint32_t b = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    return __uint_as_float(sizeof(T) == 4 ? b : e & 1 ? b & 0xffff0000u : b << 16);
+  }
+  __device__ __forceinline__ void anew() {   // the compiler keeps nothing that was made of them (10 registers of 72)
 #pragma unroll
-    for (int i = 0; i < 8 / Vec16<T>::N; ++i) Vec16<T>::unpack(u[i], v + i * Vec16<T>::N);
+    for (int i = 0; i < 8 / Vec16<T>::N; ++i) asm volatile("" : "+v"(u[i].x), "+v"(u[i].y), "+v"(u[i].z), "+v"(u[i].w));
+  }
+  __device__ __forceinline__ void clear() {   // -0, so that a sum is the other number
+    constexpr uint32_t Z = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+#pragma unroll
+    for (int i = 0; i < 8 / Vec16<T>::N; ++i) u[i] = make_uint4(Z, Z, Z, Z);
   }
 };
 
-// h 2^k (rh + rl) g to the nearest fp32 number, or (odd) where that is even and not the product, to its neighbour on the
-// product's side.
-__device__ __forceinline__ float scaled(float h, float g, int k, float rh, float rl, bool odd) {
-  h = ldexpf(h, k);
-  const float p = h * g, low = __builtin_fmaf(p, rl, __builtin_fmaf(h, g, -p) * rh), y = __builtin_fmaf(p, rh, low);
-  if (!odd) return y;
-  const float off = __builtin_fmaf(p, rh, -y) + low;
-  const uint32_t u = __float_as_uint(y);
-  const bool away = ((__float_as_uint(off) ^ u) >> 31) == 0;
-  const bool keep = (u & 1u) || !(fabsf(off) > 0.f) || !(fabsf(y) > 0.f) || fabsf(y) >= __uint_as_float(0x7f800000u);
-  return keep ? y : __uint_as_float(away ? u + 1 : u - 1);
+// y to the nearest fp32 number or, where that is even and not y, to its neighbour on y's side.
+__device__ __forceinline__ float round_odd(double y) {
+  const float f = (float)y;
+  const uint32_t u = __float_as_uint(f);
+  const bool keep = (u & 1u) || (double)f == y || !(fabsf(f) < __uint_as_float(0x7f800000u));
+  return keep ? f : __uint_as_float(fabs((double)f) < fabs(y) ? u + 1 : u - 1);
 }
 
 template <typename TS, typename T, int FMT, int NC>
@@ -225,7 +234,6 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
   if (row >= (size_t)a.rows) return;
   const TS* x = reinterpret_cast<const TS*>(a.x) + row * a.ld_x;
   const T* d = reinterpret_cast<const T*>(a.delta) + row * a.ld_delta;
-  float v[NC][8];
   Raw8<TS> xr[NC];
   Raw8<T> dr[NC], g[NC];
 #pragma unroll
@@ -234,6 +242,7 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
     if (col >= a.cols) continue;
     xr[j].load(x + col);
     if (a.delta) dr[j].load(d + col);
+    else dr[j].clear();
   }
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
@@ -245,25 +254,22 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
   for (int j = 0; j < NC; ++j) {
     const int col = (threadIdx.x + 256 * j) * 8;
     if (col >= a.cols) continue;
-    xr[j].unpack(v[j]);
-    if (a.delta) {
-      float t[8];
-      dr[j].unpack(t);
+    float h[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] += t[e];
+    for (int e = 0; e < 8; ++e) {
+      h[e] = xr[j].at(e) + dr[j].at(e);
+      const double sum = (double)xr[j].at(e) + (double)dr[j].at(e);
+      ss += sum * sum;
     }
-    if (a.h) store8(reinterpret_cast<TS*>(a.h) + row * a.ld_h + col, v[j]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss += (double)v[j][e] * (double)v[j][e];
+    if (a.h) store8(reinterpret_cast<TS*>(a.h) + row * a.ld_h + col, h);
   }
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
   __syncthreads();
   const double rs = 1.0 / sqrt((red[0] + red[1] + red[2] + red[3]) / a.cols + (double)a.eps);
-  int k;                                            // r = (rh + rl) 2^k: h 2^k is of the row's own scale
-  const double m = frexp(rs, &k);
-  const float rh = (float)m, rl = (float)(m - (double)rh);
+  const float r32 = (float)rs;
+  const uint32_t sure = r32 >= 0x1p-126f ? ~0u : 0u;   // 0: r is no normal number of fp32
   char* codes = a.operand + (size_t)tile * quads * (32 * (FMT == E2M1 ? 128 : 256));
   uint32_t* scales = reinterpret_cast<uint32_t*>(a.operand + scale_offset) + (size_t)tile * quads * 64;
 #pragma unroll
@@ -272,17 +278,16 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
     if (c >= quads * 32) continue;                  // whole groups of 32 lanes
     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // padding, also in a row of NaN
     if (c * 8 < a.cols) {
-      float t[8];
-      g[j].unpack(t);
-      uint32_t even = ~0u;                          // every border has its low 19 bits zero: few elements are near one
+      uint32_t off = sure;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        y[e] = scaled(v[j][e], t[e], k, rh, rl, false);
-        even = min(even, __float_as_uint(y[e]) & 0x7ffffu);
+        y[e] = (xr[j].at(e) + dr[j].at(e)) * r32 * g[j].at(e);
+        off = min(off, (__float_as_uint(y[e]) + 4) & 0x7ffffu);
       }
-      if (even == 0) {
+      if (off <= 8) {
+        xr[j].anew(), dr[j].anew(), g[j].anew();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = scaled(v[j][e], t[e], k, rh, rl, true);
+        for (int e = 0; e < 8; ++e) y[e] = round_odd(((double)xr[j].at(e) + (double)dr[j].at(e)) * rs * (double)g[j].at(e));
       }
     }
     put8<FMT>(codes, scales, r, c, y, true);
