@@ -81,8 +81,8 @@ int sarathi_mx_dequantize(int format, int rows, int cols, const void* operand, s
  * NULL (h = x) and h_out may be NULL (not wanted) or x itself (ld_h == ld_x);
  * otherwise h_out overlaps neither x nor delta.  h_out is the sum in fp32,
  * rounded once to its type; the norm takes the sum as it is: an element's code is that
- * of its value in 64 bits, to about 2^-45 of it.  cols is at most 24576, rows at most
- * 2^24 - 256.
+ * of its value in 64 bits, to about 2^-45 of it, from fp32's subnormal numbers to its
+ * largest (beyond: an infinity).  cols is at most 24576, rows at most 2^24 - 256.
  * A row that holds an infinity or NaN becomes NaN where the formula does.
  * Errors: as sarathi_mx_quantize; EINVAL (eps not > 0, overlaps), EUNSUPPORTED
  * (rows, cols, stream_dtype BF16 with dtype F32).

@@ -207,9 +207,9 @@ template <typename T> struct Raw8 {   // eight elements as they lie in memory
     const uint32_t b = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
     return __uint_as_float(sizeof(T) == 4 ? b : e & 1 ? b & 0xffff0000u : b << 16);
   }
-  __device__ __forceinline__ void anew() {   // the compiler keeps nothing that was made of them (10 registers of 72)
-#pragma unroll
-    for (int i = 0; i < 8 / Vec16<T>::N; ++i) asm volatile("" : "+v"(u[i].x), "+v"(u[i].y), "+v"(u[i].z), "+v"(u[i].w));
+  // The compiler keeps nothing that was made of them (bf16: 10 registers of 72).
+  __device__ __forceinline__ void anew() {
+    if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(u[0].x), "+v"(u[0].y), "+v"(u[0].z), "+v"(u[0].w));
   }
   __device__ __forceinline__ void clear() {   // -0, so that a sum is the other number
     constexpr uint32_t Z = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
@@ -267,9 +267,11 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
   for (int m = 32; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
   __syncthreads();
-  const double rs = 1.0 / sqrt((red[0] + red[1] + red[2] + red[3]) / a.cols + (double)a.eps);
+  ss = red[0] + red[1] + red[2] + red[3];
+  const double rs = 1.0 / sqrt(ss / a.cols + (double)a.eps);
   const float r32 = (float)rs;
   const uint32_t sure = r32 >= 0x1p-126f ? ~0u : 0u;   // 0: r is no normal number of fp32
+  const float low = ss > 0 ? 0x1p-100f : -1.f;         // below: h r or a block of y may have lost bits (not in rows of zeros)
   char* codes = a.operand + (size_t)tile * quads * (32 * (FMT == E2M1 ? 128 : 256));
   uint32_t* scales = reinterpret_cast<uint32_t*>(a.operand + scale_offset) + (size_t)tile * quads * 64;
 #pragma unroll
@@ -279,12 +281,16 @@ __global__ __launch_bounds__(256) void mx_norm_kernel(MxNormArgs a, int quads, s
     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // padding, also in a row of NaN
     if (c * 8 < a.cols) {
       uint32_t off = sure;
+      float least = INFINITY, most = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        y[e] = (xr[j].at(e) + dr[j].at(e)) * r32 * g[j].at(e);
+        const float t = (xr[j].at(e) + dr[j].at(e)) * r32;
+        y[e] = t * g[j].at(e);
+        least = fminf(least, fabsf(t));
+        most = fmaxf(most, fabsf(y[e]));
         off = min(off, (__float_as_uint(y[e]) + 4) & 0x7ffffu);
       }
-      if (off <= 8) {
+      if (off <= 8 || least < low || most < low) {
         xr[j].anew(), dr[j].anew(), g[j].anew();
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = round_odd(((double)xr[j].at(e) + (double)dr[j].at(e)) * rs * (double)g[j].at(e));

@@ -98,3 +98,55 @@ def test_random_rows_have_the_codes_of_64_bits(sdt, dt, fmt):
     sure = sure[..., None] & (lo_c == hi_c)
     assert sure.mean() > 1 - 1e-6
     assert np.array_equal(ref.grid(fmt)[codes][sure], ref.grid(fmt)[want_c][sure])
+
+
+@pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
+def test_small_elements_under_large_gains(fmt):
+    """Elements far below fp32's normal numbers once divided by the row's root, and gains that bring them back."""
+    rows, cols = 7, 520
+    rng = np.random.default_rng(2)
+    x = rng.standard_normal((rows, cols))
+    small = np.arange(cols) // 32 % 2 == 1
+    x = np.where(small, x * 2.0 ** -40, x * 2.0 ** 100).astype(np.float32).astype(np.float64)
+    gain = np.where(small, 2.0 ** 110, 1.0) * rng.uniform(1.0, 2.0, (1, cols))
+    gain = gain.astype(np.float32).astype(np.float64)
+    _, (codes, scales) = run_norm(rows_of(x, "f32"), None, rows_of(gain, "f32"), "f32", "f32", fmt, rows, cols, 1e-6)
+    check_exact(formula(x, gain, 1e-6), codes, scales, fmt, cols)
+
+
+@pytest.mark.parametrize("side", [-1, 1])
+@pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
+def test_borders_of_the_smallest_codes(fmt, side):
+    """Values at borders of codes of the least scale, 2^-127: subnormal numbers of fp32."""
+    rows, cols = 3, 4096
+    x = np.ones((rows, cols))
+    x[:, 32] = 0.5
+    eps = 0.75 / cols - side * 2.0 ** -30
+    gain = border_gains(fmt, cols) * 2.0 ** -127
+    gain[:, ::32] = (1.0 if fmt == "e2m1" else 64.0) * 2.0 ** -127
+    _, (codes, scales) = run_norm(rows_of(x, "f32"), None, rows_of(gain, "f32"), "f32", "f32", fmt, rows, cols, eps)
+    check_exact(formula(x, gain, eps), codes, scales, fmt, cols)
+
+
+@pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
+def test_rows_and_gains_of_the_largest_numbers(fmt):
+    rows, cols = 4, 264
+    rng = np.random.default_rng(3)
+    x = (rng.uniform(0.5, 1.0, (rows, cols)) * 3.4e38).astype(np.float32).astype(np.float64)
+    x[1] *= 2.0 ** -120
+    gain = rng.uniform(0.5, 1.0, (1, cols)) * 1.5e38
+    gain = gain.astype(np.float32).astype(np.float64)
+    _, (codes, scales) = run_norm(rows_of(x, "f32"), None, rows_of(gain, "f32"), "f32", "f32", fmt, rows, cols, 1e-6)
+    check_exact(formula(x, gain, 1e-6), codes, scales, fmt, cols)
+
+
+def test_zeros_stay_zeros_of_their_sign():
+    rows, cols = 3, 264
+    x = np.zeros((rows, cols))
+    x[1, ::2], x[2, 5:9] = -0.0, 1.0
+    gain = np.ones((1, cols))
+    gain[0, 7] = 0.0
+    for fmt in FMT:
+        h, (codes, scales) = run_norm(rows_of(x, "f32"), None, rows_of(gain, "f32"), "f32", "f32", fmt, rows, cols, 1e-6)
+        assert np.array_equal(f64(h), x) and np.array_equal(np.signbit(f64(h)), np.signbit(x))
+        check_exact(formula(x, gain, 1e-6), codes, scales, fmt, cols)
