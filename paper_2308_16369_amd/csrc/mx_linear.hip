@@ -24,8 +24,8 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 // of a dword.  The result holds column (x row) l % 32, rows (W rows) 8 g + 4 (l / 32) + i at 4 g + i.
 //
 // EXACT: the matrix cores add eight neighbouring products of e4m3 operands aligned to the largest, with 13 bits below
-// it.  The codes of exponents 8 .. 15 and those of 0 .. 7 (bit 6 of a code) span 13 bits each beside e2m1's, so in two
-// products these sums are exact.
+// it: a small product beside large ones that cancel is lost.  The codes of exponents 8 .. 15 and those of 0 .. 7 (bit 6 of a
+// code) span 13 bits each beside e2m1's, so in two products these sums are exact.
 template <int FMT, bool EXACT, int S>
 __device__ __forceinline__ floatx16 mx_mfma(const u32x4& w, uint32_t ws, const u32x4* x, uint32_t xs, floatx16 c) {
   const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
@@ -684,15 +684,19 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
   // streamed, 17.8 split; e4m3 31.2 and 18.3; 96 rows of 5120 x 8704: e2m1 13.0 and 17.0, e4m3 17.9 and 17.8).
   const bool few = w_tiles <= 256, split = few && a.quads * (long)x_tiles > (FMT == E2M1 ? 170 : 110) && a.parts && !glu;
   if (x_tiles <= 2 || (x_tiles <= 4 && few && !split)) {
+    // Up to 64 rows the sums of eight are exact whatever the output's type.  The weights' stream hides most of the second
+    // products: onto bf16, 4 rows of 15360 x 5120 take 9.6 us (11.0 with single ones), of 2 x 13824 x 5120 with SwiGLU 15.6
+    // (14.4), 64 rows of the two 17.1 (15.9) and 23.8 (21.7).
+    constexpr bool SUMS = FMT == E4M3;
     switch (x_tiles) {
       case 1:
-        if (glu) return run_stream<FMT, EXACT, 8, 2, 1>(a, s, plan);
-        return w_tiles <= 256 ? run_stream<FMT, EXACT, 16, 1, 1>(a, s, plan) : run_stream<FMT, EXACT, 8, 1, 1>(a, s, plan);
+        if (glu) return run_stream<FMT, SUMS, 8, 2, 1>(a, s, plan);
+        return w_tiles <= 256 ? run_stream<FMT, SUMS, 16, 1, 1>(a, s, plan) : run_stream<FMT, SUMS, 8, 1, 1>(a, s, plan);
       case 2:
-        if (glu) return run_stream<FMT, EXACT, 8, 2, 2>(a, s, plan);
+        if (glu) return run_stream<FMT, SUMS, 8, 2, 2>(a, s, plan);
         if constexpr (FMT == E2M1)                    // (e4m3: the registers of 16 waves do not hold a quad)
-          if (w_tiles <= 256) return run_stream<FMT, EXACT, 16, 1, 2>(a, s, plan);
-        return run_stream<FMT, EXACT, 8, 1, 2>(a, s, plan);
+          if (w_tiles <= 256) return run_stream<FMT, SUMS, 16, 1, 2>(a, s, plan);
+        return run_stream<FMT, SUMS, 8, 1, 2>(a, s, plan);
       case 3: return glu ? run_stream<FMT, EXACT, 4, 2, 3>(a, s, plan) : run_stream<FMT, EXACT, 8, 1, 3>(a, s, plan);
       default: return glu ? run_stream<FMT, EXACT, 4, 2, 4>(a, s, plan) : run_stream<FMT, EXACT, 4, 1, 4>(a, s, plan);
     }
