@@ -107,7 +107,8 @@ int sarathi_mx_norm(int stream_dtype, int dtype, int format, int rows, int cols,
  * onto bf16 go in as they are: such a sum is off by up to 8 * 2^-13 of its largest
  * product, and a product below 2^-13 of one that another cancels is lost.
  * `scratch`: as for sarathi_linear, for partial sums of split columns; with
- * NULL or less than sarathi_mx_linear_scratch_bytes(M, N) fewer splits are used.
+ * NULL or less than sarathi_mx_linear_scratch_bytes(M, N) fewer splits are used,
+ * with memory that is not 16-byte aligned none.
  * Calls that may run at once have scratch of their own.
  * Results do not depend on the order in which work runs.
  * Errors: EINVAL (NULL, sizes, kind, alignment, overlaps), EUNSUPPORTED (dtype, a_format,

@@ -680,9 +680,11 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
   const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
   const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
   // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
-  // e2m1: 9.6 us, 14 there), but not where it can split many columns of few W tiles (128 rows of 2600 x 13824: e2m1 20.7 us
+  // e2m1: 9.6 us, 14 there), but not where it splits many columns of few W tiles (128 rows of 2600 x 13824: e2m1 20.7 us
   // streamed, 17.8 split; e4m3 31.2 and 18.3; 96 rows of 5120 x 8704: e2m1 13.0 and 17.0, e4m3 17.9 and 17.8).
-  const bool few = w_tiles <= 256, split = few && a.quads * (long)x_tiles > (FMT == E2M1 ? 170 : 110) && a.parts && !glu;
+  const bool few = w_tiles <= 256, many = a.quads * (long)x_tiles > (FMT == E2M1 ? 170 : 110);
+  const TilePick pick = pick_tile(a, w_tiles, x_tiles, FMT, EXACT);
+  const bool split = few && many && pick.splits > 1;
   if (x_tiles <= 2 || (x_tiles <= 4 && few && !split)) {
     // Up to 64 rows the sums of eight are exact whatever the output's type.  The weights' stream hides most of the second
     // products: onto bf16, 4 rows of 15360 x 5120 take 9.6 us (11.0 with single ones), of 2 x 13824 x 5120 with SwiGLU 15.6
@@ -701,7 +703,6 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
       default: return glu ? run_stream<FMT, EXACT, 4, 2, 4>(a, s, plan) : run_stream<FMT, EXACT, 4, 1, 4>(a, s, plan);
     }
   }
-  const TilePick pick = pick_tile(a, w_tiles, x_tiles, FMT, EXACT);
   switch (pick.tile) {
     case 0: return run_tile<FMT, EXACT, 4, 2, 1, 1>(a, pick.splits, s, plan);
     case 1: return run_tile<FMT, EXACT, 2, 4, 2, 1>(a, pick.splits, s, plan);

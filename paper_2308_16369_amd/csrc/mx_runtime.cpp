@@ -171,8 +171,8 @@ int sarathi_mx_linear_plan(int dtype, int kind, int a_format, int M, int N, int 
   static float dummy;   // plan only: the scratch is never touched
   MxLinearArgs p{};
   p.kind = kind; p.dtype = dtype; p.M = M; p.N = N; p.quads = mx_quads(K);
-  p.parts = scratch_bytes >= 4 ? &dummy : nullptr;
   p.parts_cap = std::min(scratch_bytes / 4, mx_linear_parts(M, N));
+  p.parts = p.parts_cap ? &dummy : nullptr;
   MxLinearPlan pl{};
   if (launch_mx_linear(a_format, p, nullptr, &pl) != hipSuccess) return fail(SARATHI_EINVAL, "no plan for this op");
   *bm = pl.bm; *bn = pl.bn; *n_split = pl.splits;
@@ -212,7 +212,7 @@ int sarathi_mx_linear(int dtype, int kind, int a_format, int M, int N, int K, co
   p.up = nw;
   p.resid = resid;
   p.out = out;
-  if (scratch && aligned16(scratch)) {
+  if (scratch && parts && aligned16(scratch)) {
     p.parts = static_cast<float*>(scratch);
     p.parts_cap = parts;
   }
