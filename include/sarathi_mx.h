@@ -52,7 +52,7 @@ typedef struct {
   size_t total;                /* sarathi_mx_bytes */
 } sarathi_mx_layout;
 
-/* Bytes of an operand (0 on invalid arguments). */
+/* Bytes of an operand (0 on arguments that the operators refuse). */
 size_t sarathi_mx_bytes(int format, int rows, int cols);
 int sarathi_mx_get_layout(int format, int rows, int cols, sarathi_mx_layout* out);
 

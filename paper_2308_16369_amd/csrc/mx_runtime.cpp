@@ -76,7 +76,7 @@ int check_linear(int dtype, int kind, int a_format, int M, int N, int K) {
 extern "C" {
 
 size_t sarathi_mx_bytes(int format, int rows, int cols) {
-  return known_format(format) && sizes_fit(rows, cols) ? mx_bytes(format, rows, cols) : 0;
+  return known_format(format) && sizes_fit(rows, cols) && cols % 8 == 0 ? mx_bytes(format, rows, cols) : 0;
 }
 
 int sarathi_mx_get_layout(int format, int rows, int cols, sarathi_mx_layout* out) {

@@ -1,4 +1,4 @@
-"""The plan of a microscaled product on the host: what little scratch memory does to it."""
+"""Sizes of microscaled operands and the plan of their product on the host."""
 import pytest
 
 from paper_2308_16369_amd import sarathi as S
@@ -24,3 +24,11 @@ def test_few_w_rows_and_many_columns_split_with_scratch_and_stream_without():
     assert S.sarathi_mx_linear_plan(S.BF16, S.LINEAR_PLAIN, S.MX_E4M3, M, N, K, full)[2] > 1
     assert S.sarathi_mx_linear_plan(S.BF16, S.LINEAR_PLAIN, S.MX_E4M3, M, N, K, 16) == (96, 32, 1)
     assert S.sarathi_mx_linear_plan(S.BF16, S.LINEAR_PLAIN, S.MX_E4M3, M, N, K, 0) == (96, 32, 1)
+
+
+@pytest.mark.parametrize("fmt", [S.MX_E2M1, S.MX_E4M3])
+def test_no_bytes_for_columns_that_the_operators_refuse(fmt):
+    for cols in (1, 7, 12, 60, 257, 5121):
+        assert S.sarathi_mx_bytes(fmt, 40, cols) == 0
+        assert S.sarathi_mx_quantize(S.F32, fmt, 40, cols, 1 << 28, 8192, 2 << 28, 1 << 27, check=False) == S.EUNSUPPORTED
+    assert S.sarathi_mx_bytes(fmt, 40, 8) > 0
