@@ -73,14 +73,13 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ bool resid_f32(const MxLinearArgs& p) {
   return p.dtype == SARATHI_F32 || p.kind == SARATHI_LINEAR_RESID_F32IN;
 }
+// Two pieces of eight bytes whatever the type (bf16: the same one twice): with a branch between the types' loads the compiler
+// drains every request before each of the second type's (1955 rows of 6656 x 6656, e2m1, onto bf16: 67.7 us, 61.2 without).
 __device__ __forceinline__ uint4 load_resid4(const MxLinearArgs& p, int m, int n) {
-  const size_t at = (size_t)m * p.N + n;
-  if (resid_f32(p)) {
-    const u32x4_any r = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const float*>(p.resid) + at);
-    return make_uint4(r[0], r[1], r[2], r[3]);
-  }
-  const u32x2_any r = *reinterpret_cast<const u32x2_any*>(reinterpret_cast<const bf16*>(p.resid) + at);
-  return make_uint4(r[0], r[1], 0, 0);
+  const bool f32 = resid_f32(p);
+  const char* r = reinterpret_cast<const char*>(p.resid) + (((size_t)m * p.N + n) << (f32 ? 2 : 1));
+  const u32x2_any a = *reinterpret_cast<const u32x2_any*>(r), b = *reinterpret_cast<const u32x2_any*>(r + (f32 ? 8 : 0));
+  return make_uint4(a[0], a[1], b[0], b[1]);
 }
 __device__ __forceinline__ float4 resid4(const MxLinearArgs& p, const uint4& r) {
   if (resid_f32(p)) return __builtin_bit_cast(float4, r);
