@@ -1,11 +1,11 @@
 // Products of microscaled operands with the epilogues of the linear ops:
 //   out = epilogue(sum_b 2^(sa_b + sw_b) sum_{k in block b} a_k w_k),
 // on the matrix cores' scaled instruction, which takes both operands' codes and block scales.  Two kernels.  Up to 64 (128)
-// rows the weights stream from memory into registers as fragments: bound by that stream (4 rows of 15360 x 5120: 10.3 us,
-// 4.1 TB/s, where 2 of the 10 are the launch).  More rows run as tiles fed through LDS: bound by the matrix cores and the
-// power that they draw (probes of the loop alone reach 6.0 PFLOP/s of e2m1 on random codes, 8.9 on constant ones; 4096 rows
-// of 27648 x 5120 with SwiGLU run at 4.1 to 4.2, 273 to 285 us), and for a few hundred rows by the chain of a stage (barrier, LDS reads,
-// products) on one tile per CU.
+// rows the weights stream from memory into registers as fragments: bound by that stream (4 e4m3 rows of 15360 x 5120: 9.3 us
+// a pass, 4.5 TB/s, of which 2 us are the launch).  More rows run as tiles fed through LDS: bound by the matrix cores and the
+// power that they draw (the instruction alone, from registers, reaches 6.5 PFLOP/s of e2m1 on random codes, 8.8 on a single
+// one; 4096 rows of 27648 x 5120 with SwiGLU run at 4.1 to 4.3, 270 to 284 us by the card and the length of the run), and for
+// a few hundred rows by the chain of a stage (barrier, LDS reads, products) on one tile per CU.
 #include <algorithm>
 #include <cmath>
 
@@ -309,8 +309,8 @@ struct MxTile {
   static constexpr int PAD = 36;                                             // floats of a row of the epilogue's tile
   static constexpr int OUT = NW * 32 * PAD * 4;
   static constexpr int most(int a, int b) { return a < b ? a : b; }
-  // Whole quads, so that a stage's place goes by its place in the quad (4 or 8; with 6 the e2m1 256 x 256 tiles took 280 us
-  // where four take 257, the e4m3 256 x 128 ones 447 and 416).
+  // Whole quads, so that a stage's place goes by its place in the quad (4 or 8).  In turn on one card: 4096 rows of 27648 x
+  // 5120, e2m1, six stages 290 us, four 269 to 283; of 5120 x 13824, e4m3, 238 and 227.
   static constexpr int FIT = most(most((160 * 1024 - SR * SCALES - OUT) / STAGE, (56 - 3 * SPER) / PER), most(8, SR * SPQ));
   static constexpr int NS = FIT / 4 * 4;
   static constexpr int LDS = SR * SCALES + NS * STAGE + OUT;
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(64 * WGN * WGM, 1) void mx_tile_kernel(MxLinearArgs
     const int m0 = (at.tm * TM + wm * FM) * 32 + r0, n0 = (at.tn * WGN + wn) * FO * W + c0;
     const uint32_t put_at = out + ((le & 31) * T::PAD + 4 * (le >> 5)) * 4, get_at = out + (r0 * T::PAD + c0) * 4;
     const bool add = !GLU && splits == 1 && adds_resid(p) && p.N >= 4;
-    // The piece's residual, requested a piece ahead (1955 rows of 6656 x 6656, fp32 out, e2m1: 53.5 us, 60 without); the
+    // The piece's residual, requested a piece ahead (1955 rows of 6656 x 6656, bf16 onto fp32, e2m1: 59 us, 69 without); the
     // 256 x 256 tiles of e4m3 rows with single products have no registers left for it.
     constexpr bool AHEAD = PIECES > 1 && (FMT == E2M1 || EXACT || PIECES < 8);
     uint4 raw[ROWS];
@@ -638,8 +638,8 @@ static hipError_t run_stream(const MxLinearArgs& a, hipStream_t s, MxLinearPlan*
   return hipGetLastError();
 }
 
-// The tiles of the second kernel (W tiles by x tiles) and what 64 columns of one cost with every CU busy, in us (from 4096
-// rows of 13824 x 5120, a round of one tile per CU: e2m1 12.1, 15.5, 27, 28, 31, 37 us in the order below, e4m3 14.5, 20.5,
+// The tiles of the second kernel (W tiles by x tiles) and what 64 columns of one cost with every CU busy, in us (on one card,
+// others differ by 5 %; from 4096 rows of 13824 x 5120, a round of one tile per CU: e2m1 12.1, 15.5, 27, 28, 31, 37 us in the order below, e4m3 14.5, 20.5,
 // 31, 39.6 and 53.7, with exact sums 22, 33, 52 and 97; 2.5 of them the output's).  0: not built, another tile is
 // faster everywhere (the split of an x fragment for exact sums is shared by FN W tiles).  Where tiles leave CUs idle, the
 // columns are split: shorter tiles, but the partial sums are written and read back, and a launch of their own joins them.
@@ -679,15 +679,16 @@ static hipError_t linear_as(const MxLinearArgs& a, hipStream_t s, MxLinearPlan* 
   const bool glu = a.kind == SARATHI_LINEAR_SWIGLU;
   const int x_tiles = mx_tiles(a.M), w_tiles = (glu ? 2 : 1) * mx_tiles(a.N);
   // Up to 64 rows stream; up to 128 where the W tiles would leave CUs idle in the other kernel (128 rows of 5120 x 5120,
-  // e2m1: 9.6 us, 14 there), but not where it splits many columns of few W tiles (128 rows of 2600 x 13824: e2m1 20.7 us
-  // streamed, 17.8 split; e4m3 31.2 and 18.3; 96 rows of 5120 x 8704: e2m1 13.0 and 17.0, e4m3 17.9 and 17.8).
+  // e4m3: 12.3 us, 14.2 there; 96 rows of 5120 x 4096 9.4 and 12.8), but not where it splits many columns of few W tiles (128
+  // rows of 2600 x 13824: e4m3 23.3 us streamed, 15.9 split; e2m1 15.5 and 15.0).
   const bool few = w_tiles <= 256, many = a.quads * (long)x_tiles > (FMT == E2M1 ? 170 : 110);
   const TilePick pick = pick_tile(a, w_tiles, x_tiles, FMT, EXACT);
   const bool split = few && many && pick.splits > 1;
   if (x_tiles <= 2 || (x_tiles <= 4 && few && !split)) {
     // Up to 64 rows the sums of eight are exact whatever the output's type.  The weights' stream hides most of the second
     // products: onto bf16, 4 rows of 15360 x 5120 take 9.6 us (11.0 with single ones), of 2 x 13824 x 5120 with SwiGLU 15.6
-    // (14.4), 64 rows of the two 17.1 (15.9) and 23.8 (21.7).
+    // (14.4), 64 rows of the two 17.1 (15.9) and 23.8 (21.7); most is lost where few blocks split many columns' x: 48 rows of
+    // 5120 x 13824 17.0 (13.8).  In the other kernel exact sums take 1.7 to 2.4 times as long.
     constexpr bool SUMS = FMT == E4M3;
     switch (x_tiles) {
       case 1:

@@ -190,7 +190,8 @@ hipError_t launch_mx_dequantize(int dtype, int format, const MxQuantArgs& a, hip
 // the value in 64 bits.  (Without it one element in a million takes a border's other
 // side.)
 // Bound by the rows, x and delta read, h and e4m3 codes written: 2048 x 12288 of
-// bf16, 177 MB, in 47 us from memory (3.7 TB/s), 36 over and over (4.9 TB/s).
+// bf16, 177 MB, in 47.5 us from memory (3.7 TB/s), 37.4 over and over (4.7 TB/s); the
+// sum and the squares in fp64 are 2 of them.
 //
 // A row's output is 16-byte pieces 512 bytes apart, so the 32 rows of a tile
 // run on one XCD, one after the other, and their pieces meet in its L2 before
