@@ -105,7 +105,8 @@ int sarathi_mx_norm(int stream_dtype, int dtype, int format, int rows, int cols,
  * whatever its type, the rows go in as two parts of half the exponent range each,
  * whose sums of eight are exact (twice the matrix instructions).  More than 64 rows
  * onto bf16 go in as they are: such a sum is off by up to 8 * 2^-13 of its largest
- * product, and a product below 2^-13 of one that another cancels is lost.
+ * product, and a product below 2^-13 of one that another cancels is lost (fp32
+ * outputs are the way to exact sums of many rows).
  * `scratch`: as for sarathi_linear, for partial sums of split columns; with
  * NULL or less than sarathi_mx_linear_scratch_bytes(M, N) fewer splits are used,
  * with memory that is not 16-byte aligned none.
