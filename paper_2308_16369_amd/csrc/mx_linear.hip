@@ -59,8 +59,11 @@ __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {   // nearest eve
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
 }
 
-// silu(z) u with the hardware's reciprocal (a last place of fp32 off, where a division takes ten instructions)
-__device__ __forceinline__ float swiglu_f(float z, float u) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)) * u; }
+// silu(z) u with the hardware's reciprocal (a last place of fp32 off, where a division takes ten instructions).  It flushes
+// subnormal results, which gates below -87.3 have, so it takes 2^-24 of its operand.
+__device__ __forceinline__ float swiglu_f(float z, float u) {
+  return z * (__builtin_amdgcn_rcpf(__builtin_fmaf(__expf(-z), 0x1p-24f, 0x1p-24f)) * 0x1p-24f) * u;
+}
 
 __device__ __forceinline__ bool adds_resid(const MxLinearArgs& p) {
   return p.kind == SARATHI_LINEAR_RESID || p.kind == SARATHI_LINEAR_RESID_F32IN;

@@ -73,3 +73,28 @@ def test_products_that_cancel_leave_the_small_ones(kind, M, N):
             assert (np.abs(out - want) <= tol).all(), (dtype, float((np.abs(out - want) / tol).max()))
         else:
             assert np.array_equal(out, want), (dtype, float(np.abs(out - want).max()))
+
+
+@pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
+@pytest.mark.parametrize("M,N", [(4, 40), (100, 96), (330, 200)])
+def test_swiglu_of_far_negative_gates(fmt, M, N):
+    """Gates down to -88.6, whose silu fp32 still holds as a normal number."""
+    K = 64
+    x, w = np.zeros((M, K)), np.zeros((2 * N, K))
+    x[:, 0] = np.resize([56.0, 48.0, 40.0, 32.0] if fmt == "e4m3" else [48.0, 32.0, 24.0, 16.0], M)
+    x[:, 1] = np.resize([4.5, 4.0, 3.5] if fmt == "e4m3" else [16.0], M)
+    x[:, 32] = 1024.0
+    w[:N, 0], w[:N, 1], w[N:, 32] = -np.resize([1.5, 1.0, 0.5], N), -1.0, np.resize([6.0, -2.0, 1.0], N)
+    a, av = operand(x, fmt)
+    assert np.array_equal(av, x)
+    wt, wv = weights(w, "swiglu", N)
+    z = av @ wv.T
+    assert (z[:, :N] > -88.7).all() and (z[:, :N] < -87.4).any()
+    want = silu_product(z, N)
+    for dtype in DT:
+        out = f64(run_linear(a, wt, None, "swiglu", dtype, fmt, M, N, K))
+        half = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8
+        # the exponential of an fp32 argument, |z| steps of 2^-23, and eight more: the reciprocal's (a subnormal number of 21
+        # bits: four), the products' and the exponential's own
+        tol = np.abs(want) * ((np.abs(z[:, :N]) + 8) * 2.0 ** -23 + half)
+        assert (np.abs(out - want) <= tol).all(), (dtype, float((np.abs(out - want) / tol).max()))
