@@ -4,7 +4,7 @@
 // rows the weights stream from memory into registers as fragments: bound by that stream (4 e4m3 rows of 15360 x 5120: 9.3 us
 // a pass, 4.5 TB/s, of which 2 us are the launch).  More rows run as tiles fed through LDS: bound by the matrix cores and the
 // power that they draw (the instruction alone, from registers, reaches 6.5 PFLOP/s of e2m1 on random codes, 8.8 on a single
-// one; 4096 rows of 27648 x 5120 with SwiGLU run at 4.1 to 4.3, 270 to 284 us by the card and the length of the run), and for
+// one; 4096 rows of 27648 x 5120 with SwiGLU run at 4.1 to 4.3, 267 to 284 us by the card and the length of the run), and for
 // a few hundred rows by the chain of a stage (barrier, LDS reads, products) on one tile per CU.
 #include <algorithm>
 #include <cmath>
